@@ -272,6 +272,68 @@ int fier_decode_step_phase(const fier_config *cfg, const fier_cache *layers, int
                            size_t workspace_bytes, int32_t phase, void *stream);
 
 /*
+ * Many new tokens per sequence: prompts, chunks of prompts and drafted tokens on their way into the caches that
+ * fier_decode_step reads.  The new tokens of all sequences lie packed one after the other:
+ *   starts   [batch + 1] int32, device, ascending: sequence b's new tokens are rows starts[b] .. starts[b + 1] - 1.
+ *            Rows from starts[batch] on (a batch padded to a fixed size) are neither read nor written.  Whatever it
+ *            holds, no row outside the n_tokens is touched
+ *   n_tokens (host) rows of the arrays, at most 2^24;  max_new (host): a bound on the new tokens of any one sequence;
+ *            those past it are left out.  Both may be 0
+ *   q        [n_tokens][n_q_heads][D], k, v, k_new, v_new [n_tokens][n_kv_heads][D], device, K dtype.  Each has a stride:
+ *            the ELEMENTS from a token to the next, a multiple of 8 and at least heads * D (FIER_EALIGN, FIER_ESHAPE),
+ *            so that views of one fused projection can be passed as they are
+ *   out      [n_tokens][n_q_heads][D] in the K DTYPE (a prompt's outputs feed 16-bit products), device, contiguous
+ * Logits, softmax and sums are binary32; the weights are rounded to the K dtype for the product with V (to nearest, relative
+ * to a sum that is not), the outputs once at the end.  sm_scale must be finite (any sign).  Integer arrays are 4-byte aligned.
+ */
+
+/* Causal attention of whole prompts: token i of a sequence attends over its tokens 0 .. i.  No cache and no workspace.  Of
+ * cfg, group_size and max_ctx are only checked. */
+int fier_prefill_attn(const fier_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                      const void *v, int64_t v_stride, const int32_t *starts, int32_t n_tokens, int32_t max_new,
+                      void *out, void *stream);
+
+/* Attention of the new tokens over the cache, contiguous or paged: token i of sequence b attends over the cache's rows
+ * 0 .. seq_lens[b] + i, its own included (call fier_append_chunk first; seq_lens are the lengths before it).  Tokens past the
+ * capacity attend over all max_ctx rows.  Rows from seq_lens[b] + new tokens on are not read.  Also the form for single
+ * tokens: few rows are split over many workgroups.  workspace: fier_chunk_workspace_bytes(cfg, n_tokens, max_new); zero-filled
+ * once, it serves the other calls with this cfg too, as far as its size goes, and theirs this one. */
+int fier_chunk_attn(const fier_config *cfg, const fier_cache *cache, const void *q, int64_t q_stride,
+                    const int32_t *starts, int32_t n_tokens, int32_t max_new, void *out, void *workspace,
+                    size_t workspace_bytes, void *stream);
+size_t fier_chunk_workspace_bytes(const fier_config *cfg, int32_t n_tokens, int32_t max_new); /* 0 if invalid */
+
+/*
+ * fier_append_key for chunks.  Per sequence, write the new rows into rows seq_len .. of k / v (contiguous or paged) and extend
+ * the packed 1-bit copy over them: after the call kbits and kmeta equal fier_quantize_keys over seq_len + new tokens, bit for
+ * bit, if they held that of seq_len tokens before; kabsmax is raised.  seq_len 0 is a whole prompt (kabsmax zero-filled
+ * before).  Tokens past max_ctx are left out; seq_lens are not modified.
+ */
+int fier_append_chunk(const fier_config *cfg, const fier_cache *cache, const void *k_new, int64_t k_stride,
+                      const void *v_new, int64_t v_stride, const int32_t *starts, int32_t n_tokens, int32_t max_new,
+                      void *stream);
+
+/*
+ * The block table of a paged cache, when sequences grow, shrink (rejected drafts) or end (new length 0), all on the GPU.  All
+ * pointers device, 4-byte aligned; batch <= 16384, batch * max_ctx and n_blocks * block_tokens below 2^31 (FIER_ESHAPE).
+ *   old_lens, new_lens [batch]: tokens before and after, held to 0 .. max_ctx
+ *   table       [batch][max_ctx / block_tokens] as in fier_cache; entries 0 .. ceil(old_len / block_tokens) - 1 are in use.  A
+ *               growing sequence's new entries are filled in; the others are left as they are
+ *   free_blocks [n_blocks]: the free blocks of the pool, a stack of *n_free.  What sequences give back is pushed (sequences,
+ *               then entries ascending), what they need popped afterwards (in the same order)
+ *   n_free_out  (not n_free) receives how many are free afterwards.  If that is negative there are as many too few: then
+ *               nothing else is written
+ *   starts      optional [batch + 1]: packed offsets of the tokens by which sequences grow, as the calls above take them
+ *   slots       optional (with starts) [n_slots]: for every such token the row table[...] * block_tokens + position in the
+ *               block; those past n_slots are left out, further entries left as they are
+ * Only new entries of growing sequences and places of free_blocks from *n_free on are written, and neither is read: the call
+ * may be repeated.
+ */
+int fier_block_table(const fier_config *cfg, int32_t block_tokens, const int32_t *old_lens, const int32_t *new_lens,
+                     int32_t *table, int32_t *free_blocks, int32_t n_blocks, const int32_t *n_free, int32_t *n_free_out,
+                     int32_t *starts, int32_t *slots, int32_t n_slots, void *stream);
+
+/*
  * Page-level importance, the page-retrieval baseline the paper compares with (Sec. 3.2, Eq. 1-3) and the
  * "averaged quantized score per page" ablation of Sec. 4.4: a second workload for fier_topk and fier_sparse_attn.
  * A page = page_tokens (8, 16 or 32) consecutive tokens of a unit.

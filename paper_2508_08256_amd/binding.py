@@ -24,7 +24,8 @@ SYMBOLS = ["fier_packed_bits_bytes", "fier_packed_meta_bytes", "fier_workspace_b
            "fier_sparse_attn", "fier_dense_attn", "fier_decode_step", "fier_decode_step_static", "fier_decode_step_mixed", "fier_decode_step_phase",
            "fier_decode_step_kernels", "fier_page_meta_bytes",
            "fier_page_minmax", "fier_page_append", "fier_page_score", "fier_page_mean_score", "fier_expand_pages", "fier_unpack_bits",
-           "fier_unpack_meta"]
+           "fier_unpack_meta", "fier_prefill_attn", "fier_chunk_attn", "fier_chunk_workspace_bytes", "fier_append_chunk",
+           "fier_block_table"]
 
 
 class FierError(RuntimeError):
@@ -122,6 +123,17 @@ def lib():
         L.fier_decode_step_mixed.argtypes = [cfgp, cachep, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, C.c_size_t, vp]
         L.fier_decode_step_phase.restype = C.c_int
         L.fier_decode_step_phase.argtypes = [cfgp, cachep, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, C.c_size_t, i32, vp]
+        i64 = C.c_int64
+        L.fier_prefill_attn.restype = C.c_int
+        L.fier_prefill_attn.argtypes = [cfgp, vp, i64, vp, i64, vp, i64, vp, i32, i32, vp, vp]
+        L.fier_chunk_attn.restype = C.c_int
+        L.fier_chunk_attn.argtypes = [cfgp, cachep, vp, i64, vp, i32, i32, vp, vp, C.c_size_t, vp]
+        L.fier_chunk_workspace_bytes.restype = C.c_size_t
+        L.fier_chunk_workspace_bytes.argtypes = [cfgp, i32, i32]
+        L.fier_append_chunk.restype = C.c_int
+        L.fier_append_chunk.argtypes = [cfgp, cachep, vp, i64, vp, i64, vp, i32, i32, vp]
+        L.fier_block_table.restype = C.c_int
+        L.fier_block_table.argtypes = [cfgp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp]
         L.fier_unpack_bits.restype = None
         L.fier_unpack_bits.argtypes = [cfgp, vp, vp]
         L.fier_unpack_meta.restype = None
@@ -369,3 +381,71 @@ def decode_step_phase(cfg: Config, caches, q, k_new, v_new, budgets, max_budget:
     _check(lib().fier_decode_step_phase(C.byref(cfg), arr, len(caches), _ptr(q), _ptr(k_new), _ptr(v_new),
                                         _ptr(budgets), int(max_budget), _ptr(out), _ptr(idx_out), _ptr(count_out),
                                         *_ws(workspace), int(phase), _stream()), "fier_decode_step_phase")
+
+
+def _rows(t, heads: int, head_dim: int, n: int, what: str):
+    """(pointer, elements from a token to the next) of a tensor [n][heads][head_dim] whose tokens may lie apart."""
+    s = t.stride()
+    if tuple(t.shape) != (n, heads, head_dim) or t.element_size() != 2 or s[2] != 1 or (heads > 1 and s[1] != head_dim):
+        raise FierError(ESHAPE, f"{what}: {tuple(t.shape)}, strides {s}, of {n} tokens")
+    return t.data_ptr(), s[0] if n > 1 else max(s[0], heads * head_dim)  # a single row's stride may be anything
+
+
+def prefill_attn(cfg: Config, q, k, v, starts, max_new: int, out):
+    """q, out [n_tokens][n_q_heads][128], k, v [n_tokens][n_kv_heads][128] (out contiguous, the others may be views of a fused
+    projection); starts [batch + 1] int32."""
+    n, d = q.shape[0], cfg.head_dim
+    out_p, out_stride = _rows(out, cfg.n_q_heads, d, n, "out")
+    if out_stride != cfg.n_q_heads * d:
+        raise FierError(ESHAPE, "out: not contiguous")
+    _check(lib().fier_prefill_attn(C.byref(cfg), *_rows(q, cfg.n_q_heads, d, n, "q"), *_rows(k, cfg.n_kv_heads, d, n, "k"),
+                                   *_rows(v, cfg.n_kv_heads, d, n, "v"), _ptr(starts), n, int(max_new), out_p, _stream()),
+           "fier_prefill_attn")
+
+
+def chunk_workspace_bytes(cfg: Config, n_tokens: int, max_new: int) -> int:
+    return int(lib().fier_chunk_workspace_bytes(C.byref(cfg), int(n_tokens), int(max_new)))
+
+
+def make_chunk_workspace(cfg: Config, n_tokens: int, max_new: int):
+    """A zero-filled workspace on the GPU for chunk_attn calls of up to n_tokens rows and max_new tokens of a sequence."""
+    import torch
+
+    n = chunk_workspace_bytes(cfg, n_tokens, max_new)
+    assert n > 0
+    return torch.zeros(n, dtype=torch.uint8, device="cuda")
+
+
+def chunk_attn(cfg: Config, cache: DeviceCache, q, starts, max_new: int, out, workspace):
+    n, d = q.shape[0], cfg.head_dim
+    out_p, out_stride = _rows(out, cfg.n_q_heads, d, n, "out")
+    if out_stride != cfg.n_q_heads * d:
+        raise FierError(ESHAPE, "out: not contiguous")
+    _check(lib().fier_chunk_attn(C.byref(cfg), C.byref(cache.c), *_rows(q, cfg.n_q_heads, d, n, "q"), _ptr(starts), n,
+                                 int(max_new), out_p, *_ws(workspace), _stream()), "fier_chunk_attn")
+
+
+def append_chunk(cfg: Config, cache: DeviceCache, k_new, v_new, starts, max_new: int):
+    """k_new, v_new [n_tokens][n_kv_heads][128], possibly views; starts [batch + 1] int32."""
+    n, d = k_new.shape[0], cfg.head_dim
+    _check(lib().fier_append_chunk(C.byref(cfg), C.byref(cache.c), *_rows(k_new, cfg.n_kv_heads, d, n, "k_new"),
+                                   *_rows(v_new, cfg.n_kv_heads, d, n, "v_new"), _ptr(starts), n, int(max_new), _stream()),
+           "fier_append_chunk")
+
+
+def block_table(cfg: Config, block_tokens: int, old_lens, new_lens, table, free_blocks, n_free, n_free_out, starts=None,
+                slots=None):
+    """int32 tensors on the GPU: old_lens, new_lens [batch], table [batch][max_ctx / block_tokens], free_blocks [pool blocks],
+    n_free, n_free_out of one element, starts [batch + 1], slots of any size."""
+    import torch
+
+    ints = (old_lens, new_lens, table, free_blocks, n_free, n_free_out, starts, slots)
+    if any(t is not None and (t.dtype != torch.int32 or not t.is_contiguous()) for t in ints):
+        raise FierError(EINVAL, "fier_block_table: contiguous int32 tensors are wanted")
+    if (old_lens.numel() != cfg.batch or new_lens.numel() != cfg.batch or block_tokens < 1
+            or table.numel() != cfg.batch * (cfg.max_ctx // block_tokens)
+            or (starts is not None and starts.numel() < cfg.batch + 1)):
+        raise FierError(ESHAPE, "fier_block_table")
+    _check(lib().fier_block_table(C.byref(cfg), int(block_tokens), _ptr(old_lens), _ptr(new_lens), _ptr(table),
+                                  _ptr(free_blocks), free_blocks.numel(), _ptr(n_free), _ptr(n_free_out), _ptr(starts),
+                                  _ptr(slots), 0 if slots is None else slots.numel(), _stream()), "fier_block_table")

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 
 #include "fier.h"
@@ -585,6 +586,131 @@ int fier_decode_step_static(const fier_config* cfg, const fier_cache* layers, in
     return FIER_EHIP;
   return decode_step_impl(cfg, layers, n_layers, nullptr, q, k_new, v_new, budgets, max_budget, out, idx_out, count_out,
                           ptr, kStaticScratchBytes, 0, stream);
+}
+
+// ---- many new tokens per sequence -----------------------------------------------------------------------------------
+// q, k, v rows as the caller's projections left them: `stride` elements from a token to the next, its heads side by side.
+static int check_rows(const void* p, int64_t stride, int heads) {
+  if (stride < (int64_t)heads * kD || stride > (int64_t)1 << 40) return FIER_ESHAPE;
+  return misaligned(p) || stride % 8 != 0 ? FIER_EALIGN : FIER_OK;
+}
+constexpr int32_t kMaxNewTokens = 1 << 24;  // rows of the new tokens: query rows of a unit then fit 32 bits
+static int check_new(const fier_config* cfg, const int32_t* starts, int32_t n_tokens, int32_t max_new) {
+  const int st = check_cfg(cfg);
+  if (st != FIER_OK) return st;
+  if (!starts || n_tokens < 0 || max_new < 0) return FIER_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(starts) & 3u) != 0) return FIER_EALIGN;
+  return n_tokens > kMaxNewTokens ? FIER_ESHAPE : FIER_OK;
+}
+
+static fier::PromptArgs prompt_args(const fier_config* cfg, const void* q, int64_t q_stride, const int32_t* starts,
+                                    int32_t n_tokens, int32_t max_new, void* out) {
+  fier::PromptArgs a = {};
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.q_stride = 2 * q_stride;
+  a.starts = starts;
+  // scale = |sm_scale| log2(e); the sign goes to the queries, and a scale of zero makes them zero
+  a.scale = cfg->sm_scale == 0.f ? 1.f : std::fabs(cfg->sm_scale) * 1.4426950408889634f;
+  a.flip = cfg->sm_scale < 0.f ? 0x80008000u : 0u;
+  a.keep = cfg->sm_scale == 0.f ? 0u : 0xffffffffu;
+  a.units = units_of(cfg);
+  a.n_kv_heads = cfg->n_kv_heads;
+  a.n_q_heads = cfg->n_q_heads;
+  a.n_rep = n_rep_of(cfg);
+  a.n_tokens = n_tokens;
+  a.max_new = std::min(max_new, n_tokens);
+  a.kv_cap = INT32_MAX;
+  return a;
+}
+
+int fier_prefill_attn(const fier_config* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                      const void* v, int64_t v_stride, const int32_t* starts, int32_t n_tokens, int32_t max_new, void* out,
+                      void* stream) {
+  int st = check_new(cfg, starts, n_tokens, max_new);
+  if (st != FIER_OK) return st;
+  if ((n_tokens && (!q || !k || !v || !out)) || !std::isfinite(cfg->sm_scale)) return FIER_EINVAL;
+  if (misaligned(out)) return FIER_EALIGN;
+  for (int rc : {check_rows(q, q_stride, cfg->n_q_heads), check_rows(k, k_stride, cfg->n_kv_heads),
+                 check_rows(v, v_stride, cfg->n_kv_heads)})
+    if (rc != FIER_OK) return rc;
+  fier::PromptArgs a = prompt_args(cfg, q, q_stride, starts, n_tokens, max_new, out);
+  a.k = static_cast<const char*>(k), a.v = static_cast<const char*>(v);
+  a.k_stride = 2 * k_stride, a.v_stride = 2 * v_stride;
+  return fier::launch_prompt_attn(cfg->kv_dtype, a, (hipStream_t)stream);
+}
+
+int fier_chunk_attn(const fier_config* cfg, const fier_cache* cache, const void* q, int64_t q_stride, const int32_t* starts,
+                    int32_t n_tokens, int32_t max_new, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_new(cfg, starts, n_tokens, max_new);
+  if (st != FIER_OK) return st;
+  st = check_cache(cfg, cache);
+  if (st != FIER_OK) return st;
+  if ((n_tokens && (!q || !out)) || !std::isfinite(cfg->sm_scale)) return FIER_EINVAL;
+  if (misaligned(out)) return FIER_EALIGN;
+  st = check_rows(q, q_stride, cfg->n_q_heads);
+  if (st != FIER_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, fier_chunk_workspace_bytes(cfg, n_tokens, max_new));
+  if (st != FIER_OK) return st;
+  fier::PromptArgs a = prompt_args(cfg, q, q_stride, starts, n_tokens, max_new, out);
+  a.k = static_cast<const char*>(cache->k), a.v = static_cast<const char*>(cache->v);
+  a.k_stride = a.v_stride = 2 * kD;
+  a.seq_lens = cache->seq_lens;
+  a.lay = layout_of(cfg, cache);
+  a.kv_cap = cfg->max_ctx;
+  a.from_cache = true;
+  return fier::launch_prompt_attn(cfg->kv_dtype, a, (hipStream_t)stream);
+}
+
+size_t fier_chunk_workspace_bytes(const fier_config* cfg, int32_t n_tokens, int32_t max_new) {
+  if (check_cfg(cfg) != FIER_OK || n_tokens < 0 || n_tokens > kMaxNewTokens || max_new < 0) return 0;
+  return carve(cfg, 1, nullptr).zero_bytes;
+}
+
+int fier_append_chunk(const fier_config* cfg, const fier_cache* cache, const void* k_new, int64_t k_stride,
+                      const void* v_new, int64_t v_stride, const int32_t* starts, int32_t n_tokens, int32_t max_new,
+                      void* stream) {
+  int st = check_new(cfg, starts, n_tokens, max_new);
+  if (st != FIER_OK) return st;
+  st = check_cache(cfg, cache);
+  if (st != FIER_OK) return st;
+  if (n_tokens && (!k_new || !v_new)) return FIER_EINVAL;
+  for (int rc : {check_rows(k_new, k_stride, cfg->n_kv_heads), check_rows(v_new, v_stride, cfg->n_kv_heads)})
+    if (rc != FIER_OK) return rc;
+  fier::NewRows src = {};
+  src.k = static_cast<const char*>(k_new), src.v = static_cast<const char*>(v_new);
+  src.k_stride = 2 * k_stride, src.v_stride = 2 * v_stride;
+  src.starts = starts;
+  src.n_tokens = n_tokens;
+  src.max_new = std::min(max_new, n_tokens);
+  src.V = cache->v;
+  if (src.max_new == 0) return FIER_OK;
+  return hip_status(fier::launch_append_chunk(cfg->kv_dtype, layout_of(cfg, cache), cache->k, cache->kbits, cache->kmeta,
+                                              cache->kabsmax, cache->seq_lens, src, units_of(cfg), cfg->n_kv_heads,
+                                              cfg->max_ctx, cfg->group_size, (hipStream_t)stream));
+}
+
+int fier_block_table(const fier_config* cfg, int32_t block_tokens, const int32_t* old_lens, const int32_t* new_lens,
+                     int32_t* table, int32_t* free_blocks, int32_t n_blocks, const int32_t* n_free, int32_t* n_free_out,
+                     int32_t* starts, int32_t* slots, int32_t n_slots, void* stream) {
+  int st = check_cfg(cfg);
+  if (st != FIER_OK) return st;
+  if (!old_lens || !new_lens || !table || (!free_blocks && n_blocks) || !n_free || !n_free_out || n_blocks < 0 || n_slots < 0)
+    return FIER_EINVAL;
+  if (n_free == n_free_out || old_lens == new_lens || (slots && !starts) || (!slots && n_slots)) return FIER_EINVAL;
+  const fier_cache rows = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, table, block_tokens};
+  st = check_blocks(cfg, &rows);
+  if (st != FIER_OK) return st;
+  for (const void* p : {(const void*)old_lens, (const void*)new_lens, (const void*)free_blocks, (const void*)n_free,
+                        (const void*)n_free_out, (const void*)starts, (const void*)slots})
+    if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return FIER_EALIGN;
+  // offsets and slots are 32-bit numbers; the sums over the batch lie in 64 KiB of shared memory
+  if (cfg->batch > 16384 || (int64_t)cfg->batch * cfg->max_ctx > INT32_MAX || (int64_t)n_blocks * block_tokens > INT32_MAX)
+    return FIER_ESHAPE;
+  int shift = 0;
+  while ((1 << shift) < block_tokens) ++shift;
+  return hip_status(fier::launch_block_table(shift, cfg->max_ctx, cfg->batch, old_lens, new_lens, table, free_blocks, n_blocks,
+                                             n_free, n_free_out, starts, slots, n_slots, (hipStream_t)stream));
 }
 
 // ---- page-level importance ------------------------------------------------------------------------------------------

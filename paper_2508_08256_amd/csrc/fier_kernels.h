@@ -138,6 +138,22 @@ hipError_t launch_append(int dtype, KvLayout lay, void* K, void* V, uint32_t* kb
                          const int32_t* seq_lens, const void* k_new, const void* v_new, int units, int n_kv_heads,
                          int max_ctx, int group_size, hipStream_t st);
 
+// Where the rows of a quantization come from: the cache, or a chunk of new tokens on their way into it.
+struct CachedRows {
+  static constexpr int n_copy = 1;  // not used
+};
+struct NewRows {
+  const char *k, *v;          // packed rows of the new tokens
+  int64_t k_stride, v_stride;  // bytes from a token to the next
+  const int32_t* starts;       // sequence b's new tokens: rows starts[b] .. starts[b + 1] - 1
+  int n_tokens, max_new;
+  void* V;     // the cache's V
+  int n_copy;  // workgroups per unit that copy V rows (set by the launcher)
+};
+hipError_t launch_append_chunk(int dtype, KvLayout lay, void* K, uint32_t* kbits, uint32_t* kmeta, float* kabsmax,
+                               const int32_t* seq_lens, NewRows src, int units, int n_kv_heads, int max_ctx, int group_size,
+                               hipStream_t st);
+
 // With sb != nullptr the kernel also builds the per-unit score histogram (first kernel of the fused step); with
 // k_new != nullptr as well it appends the new K/V rows first (extra must then be 1).
 hipError_t launch_score(int dtype, KvLayout lay, int n_rep, const uint32_t* kbits, const uint32_t* kmeta, const float* kabsmax,
@@ -195,6 +211,42 @@ hipError_t launch_attn(int dtype, KvLayout lay, int n_rep, const void* K, const 
                        const int32_t* count, const int32_t* seq_lens, int extra, int max_budget, int rows_per_wg,
                        int n_splits, float sm_scale, float* po, float* pm, float* pl, UnitCtl* ctl, float* out, int units,
                        int n_kv_heads, int max_ctx, hipStream_t st);
+
+// ---- many new tokens per sequence ----------------------------------------------------------------------------------------
+hipError_t launch_block_table(int block_shift, int max_ctx, int batch, const int32_t* old_lens, const int32_t* new_lens,
+                              int32_t* table, int32_t* free_blocks, int n_blocks, const int32_t* n_free, int32_t* n_free_out,
+                              int32_t* starts, int32_t* slots, int n_slots, hipStream_t st);
+
+struct PromptSpan {
+  int lo, n;  // the sequence's new tokens: rows lo .. lo + n - 1 of q and out (and of k and v where they are packed)
+  int first;  // rows in front of them that they attend over too
+};
+struct PromptArgs {  // attention of the new tokens (passed to the kernel by value)
+  const char *q, *k, *v;  // k, v: a cache's arrays if from_cache, else packed rows of the new tokens
+  char* out;
+  int64_t q_stride, k_stride, v_stride;  // bytes from a token to the next (cache: from a row to the next)
+  const int32_t *starts, *seq_lens;      // seq_lens: nullptr without a cache
+  KvLayout lay;
+  float scale;   // softmax scale * log2(e), positive
+  uint32_t flip, keep;  // sign bits to flip (negative scales) and bits to keep (none for a scale of 0) of the queries
+  int units, n_kv_heads, n_q_heads, n_rep;
+  int n_tokens, max_new, kv_cap;  // kv_cap: rows of a cache; no limit without one
+  int row_tiles;
+  bool from_cache;
+  // Whatever the offsets hold, the span lies inside the n_tokens rows.
+  __device__ __forceinline__ PromptSpan span(int b) const {
+    const int lo = max(0, min(starts[b], n_tokens)), hi = max(lo, min(starts[b + 1], n_tokens));
+    const int first = seq_lens ? max(0, min(seq_lens[b], kv_cap)) : 0;
+    return {lo, min(hi - lo, max_new), first};
+  }
+  __device__ __forceinline__ uint4 load_q(const char* p) const {
+    uint4 w = *reinterpret_cast<const uint4*>(p);
+    w.x = (w.x ^ flip) & keep, w.y = (w.y ^ flip) & keep, w.z = (w.z ^ flip) & keep, w.w = (w.w ^ flip) & keep;
+    return w;
+  }
+};
+// FIER_OK, FIER_EHIP, or FIER_ESHAPE for a grid that does not fit 32 bits.
+int launch_prompt_attn(int dtype, PromptArgs a, hipStream_t st);
 
 // ---- page-level importance (comparison workload) -------------------------------------------------------------------
 hipError_t launch_page_minmax(int dtype, KvLayout lay, const void* K, const int32_t* seq_lens, uint32_t* page_meta, int units,

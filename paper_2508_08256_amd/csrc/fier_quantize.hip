@@ -8,6 +8,9 @@
 // The decision arithmetic is fixed so that any implementation of the same definition produces the
 // same bits:  z = min (an input value, -0 -> +0);  s = RN_dtype(f32(max) - f32(z)), held at the
 // largest finite value;  bit = 2*(f32(k) - f32(z)) >= f32(s);  all in binary32, no contraction.
+#include <algorithm>
+#include <type_traits>
+
 #include "fier_dev.h"
 #include "fier_kernels.h"
 #include "fier_quant_dev.h"
@@ -27,14 +30,12 @@ __device__ __forceinline__ short2_t order_keys(uint32_t pair) {
   return v ^ ((v >> 15) & (short)0x7fff);
 }
 
-// One wavefront, g = 32: the unit's last pair block when it is partial (1 to 63 tokens present).
-template <int DT>
-__device__ __forceinline__ void quantize_tail_short(const uint32_t* __restrict__ K, uint32_t* __restrict__ kbits,
-                                                    uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax,
-                                                    const int32_t* __restrict__ seq_lens, int n_kv_heads, int max_ctx,
-                                                    const KvLayout& lay, const int unit, const int lane) {
-  int L = seq_lens[unit / n_kv_heads];
-  L = L < 0 ? 0 : (L > max_ctx ? max_ctx : L);
+// One wavefront, g = 32: the unit's last pair block when it is partial (1 to 63 tokens present).  rows_from(t0)(t): the lane's
+// channel pair of token t0 + t, both in one group.
+template <int DT, class RowsFrom>
+__device__ __forceinline__ void quantize_tail_short(RowsFrom rows_from, uint32_t* __restrict__ kbits,
+                                                    uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax, int L,
+                                                    int max_ctx, const int unit, const int lane) {
   const int P = L / kPair;
   if (P * kPair >= L) return;
   const int n_groups = max_ctx / kG;
@@ -48,9 +49,9 @@ __device__ __forceinline__ void quantize_tail_short(const uint32_t* __restrict__
     uint32_t meta0 = 0, meta1 = 0;
     if (ntok > 0) {
       uint32_t rows[kG];
-      const uint32_t* src = K + lay.rows_of(unit).row(t0) * (kD / 2) + lane;
+      const auto row_at = rows_from(t0);
 #pragma unroll
-      for (int t = 0; t < kG; ++t) rows[t] = src[(size_t)(t < ntok ? t : 0) * (kD / 2)];
+      for (int t = 0; t < kG; ++t) rows[t] = row_at(t < ntok ? t : 0);
       const GroupScale gs = quantize_group<DT>(rows, ntok, lane, h * kG, mine);
       meta0 = gs.s0 | (gs.z0 << 16);
       meta1 = gs.s1 | (gs.z1 << 16);
@@ -67,21 +68,17 @@ __device__ __forceinline__ void quantize_tail_short(const uint32_t* __restrict__
 
 // One wavefront, g = 32 ns with ns in {2, 4, 8}: the unit's last group when it is partial.  Its rows are read twice
 // (min / max, then codes), 32 at a time.
-template <int DT>
-__device__ __forceinline__ void quantize_tail_long(const uint32_t* __restrict__ K, uint32_t* __restrict__ kbits,
-                                                   uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax,
-                                                   const int32_t* __restrict__ seq_lens, int n_kv_heads, int max_ctx,
-                                                   int ns, const KvLayout& lay, const int unit, const int lane) {
+template <int DT, class RowsFrom>
+__device__ __forceinline__ void quantize_tail_long(RowsFrom rows_from, uint32_t* __restrict__ kbits,
+                                                   uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax, int L,
+                                                   int max_ctx, int ns, const int unit, const int lane) {
   const int g = kG * ns;
-  int L = seq_lens[unit / n_kv_heads];
-  L = L < 0 ? 0 : (L > max_ctx ? max_ctx : L);
   const int Gi = L / g;
   const int t0 = Gi * g;
   if (t0 >= L) return;
   const int ntok = L - t0;
   const int n_groups = max_ctx / g;
-  const uint32_t* src = K + lay.rows_of(unit).row(t0) * (kD / 2) + lane;
-  auto row_at = [&](int t) { return src[(size_t)t * (kD / 2)]; };
+  const auto row_at = rows_from(t0);
   const GroupScale gs = long_group_scale<DT>(row_at, ntok);
   uint2* mdst = reinterpret_cast<uint2*>(kmeta + ((size_t)unit * n_groups + Gi) * kD) + lane;
   *mdst = make_uint2(gs.s0 | (gs.z0 << 16), gs.s1 | (gs.z1 << 16));
@@ -105,15 +102,14 @@ __device__ __forceinline__ void quantize_tail_long(const uint32_t* __restrict__ 
   raise_absmax(kabsmax + (size_t)unit * kD + 2 * lane + 1, gs.amax1());
 }
 
-template <int DT, int NS>
-__device__ __forceinline__ void quantize_tail(const uint32_t* __restrict__ K, uint32_t* __restrict__ kbits,
-                                              uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax,
-                                              const int32_t* __restrict__ seq_lens, int n_kv_heads, int max_ctx,
-                                              const KvLayout& lay, const int unit, const int lane) {
+template <int DT, int NS, class RowsFrom>
+__device__ __forceinline__ void quantize_tail(RowsFrom rows_from, uint32_t* __restrict__ kbits, uint32_t* __restrict__ kmeta,
+                                              float* __restrict__ kabsmax, int L, int max_ctx, const int unit,
+                                              const int lane) {
   if constexpr (NS == 1)
-    quantize_tail_short<DT>(K, kbits, kmeta, kabsmax, seq_lens, n_kv_heads, max_ctx, lay, unit, lane);
+    quantize_tail_short<DT>(rows_from, kbits, kmeta, kabsmax, L, max_ctx, unit, lane);
   else
-    quantize_tail_long<DT>(K, kbits, kmeta, kabsmax, seq_lens, n_kv_heads, max_ctx, NS, lay, unit, lane);
+    quantize_tail_long<DT>(rows_from, kbits, kmeta, kabsmax, L, max_ctx, NS, unit, lane);
 }
 
 // The same word by word for one 16-bit float; keys order like the floats, -0 (key -1) just below +0 (key 0).
@@ -259,37 +255,98 @@ __device__ __forceinline__ uint32_t transpose_nibbles(uint32_t v, uint32_t sel4,
 // pair per lane and made each row's two ballots into a code word, took 71 us there, 50 of them the issue of 27 vector
 // instructions per row; this one issues 9 (fp16) and 12 (bf16).  32 x 128k: 284 -> 230 us; 32 ragged units up to 24k at
 // g = 128: 74 -> 35.  128 registers keep four workgroups on a CU.
-template <int DT, int NS>
-__global__ __launch_bounds__(256, 4) void quantize_kernel(const uint32_t* __restrict__ K, uint32_t* __restrict__ kbits,
+//   Rows = NewRows: the same for a chunk of new tokens, from the first group that one of them falls in on.  A row is read from
+// the chunk, or from the cache where it was there before, and a new K row is stored in the cache from the registers it is
+// coded from; the V rows are copied by workgroups of their own at the end of the grid, a wavefront 16 tokens a time.
+template <int DT, int NS, class Rows>
+__global__ __launch_bounds__(256, 4) void quantize_kernel(uint32_t* __restrict__ K, uint32_t* __restrict__ kbits,
                                                        uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax,
                                                        const int32_t* __restrict__ seq_lens, int units, int n_kv_heads,
-                                                       int max_ctx, int bpw, int n_x, KvLayout lay) {
+                                                       int max_ctx, int bpw, int n_x, KvLayout lay, Rows src) {
   using P16 = Pair16<DT>;
+  constexpr bool kNew = std::is_same_v<Rows, NewRows>;
   constexpr int kWavesPerGroup = NS >= 4 ? NS / 2 : 1;
   __shared__ uint2 xch[2][4][64];  // [iteration parity][wavefront][lane]: packed (min, max), NS >= 4 only
   const int lane = threadIdx.x & 63;
   // the wavefront's number as a scalar: everything derived from it (addresses, branches) is then uniform for the
   // compiler too
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((int)blockIdx.x < units) {
-    if (wave == 0) quantize_tail<DT, NS>(K, kbits, kmeta, kabsmax, seq_lens, n_kv_heads, max_ctx, lay, (int)blockIdx.x, lane);
-    return;
-  }
+  const int n_quant = units * (1 + n_x);
   const int wid = (int)blockIdx.x - units;
-  const int unit = wid / n_x;
-  const int base = (wid - unit * n_x) * (4 * bpw);
+  const int unit = kNew && (int)blockIdx.x >= n_quant ? ((int)blockIdx.x - n_quant) / src.n_copy
+                                                      : (wid < 0 ? (int)blockIdx.x : wid / n_x);
   int L = seq_lens[unit / n_kv_heads];
   L = L < 0 ? 0 : (L > max_ctx ? max_ctx : L);
+  const int L0 = L;  // tokens in the cache before a chunk
+  const KvRows kv = lay.rows_of(unit);
+  const char *kn = nullptr, *vn = nullptr;  // the chunk's rows of this head, moved to where token 0 would be
+  if constexpr (kNew) {
+    const int b = unit / n_kv_heads, head = unit - b * n_kv_heads;
+    const int lo = max(0, min(src.starts[b], src.n_tokens)), hi = max(lo, min(src.starts[b + 1], src.n_tokens));
+    L = min(L0 + min(hi - lo, src.max_new), max_ctx);
+    if (L == L0) return;
+    kn = src.k + (int64_t)(lo - L0) * src.k_stride + head * (kD * 2);
+    vn = src.v + (int64_t)(lo - L0) * src.v_stride + head * (kD * 2);
+    if ((int)blockIdx.x >= n_quant) {
+      // 64 tokens of V: token t0 + 16 i + 4 wave + lane / 16, a multiple of 64 at the start
+      const int t0 = (L0 / kPair + ((int)blockIdx.x - n_quant) % src.n_copy) * kPair;
+      if (t0 >= L) return;
+      uint4 w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = t0 + 16 * i + 4 * wave + (lane >> 4);
+        w[i] = load_stream(reinterpret_cast<const uint4*>(vn + (int64_t)max(L0, min(t, L - 1)) * src.v_stride) + (lane & 15));
+      }
+      uint4* const dst = reinterpret_cast<uint4*>(src.V) + kv.row(t0) * (kD / 8) + (lane & 15);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = 16 * i + 4 * wave + (lane >> 4);
+        if (t0 + t >= L0 && t0 + t < L) dst[t * (kD / 8)] = w[i];
+      }
+      return;
+    }
+  }
   // pair blocks that consist of whole groups
   const int n_full = NS == 1 ? L / kPair : (L / (kG * NS)) * (NS / 2);
+  if (wid < 0) {
+    if constexpr (kNew) {
+      // the K rows behind the whole groups; the wavefront that codes them reads them from the chunk
+      for (int t = max(L0, n_full * kPair) + 4 * wave + (lane >> 4); t < L; t += 16)
+        reinterpret_cast<uint4*>(K)[kv.row(t) * (kD / 8) + (lane & 15)] =
+            reinterpret_cast<const uint4*>(kn + (int64_t)t * src.k_stride)[lane & 15];
+      if (wave == 0)
+        quantize_tail<DT, NS>(
+            [&](int t0) {
+              const uint32_t* old = K + kv.row(t0) * (kD / 2) + lane;
+              return [=](int t) {
+                return t0 + t < L0 ? old[(size_t)t * (kD / 2)]
+                                   : reinterpret_cast<const uint32_t*>(kn + (int64_t)(t0 + t) * src.k_stride)[lane];
+              };
+            },
+            kbits, kmeta, kabsmax, L, max_ctx, unit, lane);
+    } else if (wave == 0) {
+      quantize_tail<DT, NS>(
+          [&](int t0) {
+            const uint32_t* rows = K + kv.row(t0) * (kD / 2) + lane;
+            return [=](int t) { return rows[(size_t)t * (kD / 2)]; };
+          },
+          kbits, kmeta, kabsmax, L, max_ctx, unit, lane);
+    }
+    return;
+  }
+  const int base = (wid - unit * n_x) * (4 * bpw) + (kNew ? L0 / (NS == 1 ? kPair : kG * NS) * (NS == 1 ? 1 : NS / 2) : 0);
   if (base >= n_full) return;
   const int n_groups = max_ctx / (kG * NS);
-  const KvRows kv = lay.rows_of(unit);
   const int r = lane >> 4, n = lane & 15;
   // row i of the lane: uniform block address + the lane's offset + 256 i
-  const char* const K1 = reinterpret_cast<const char*>(K);
+  char* const K1 = reinterpret_cast<char*>(K);
   uint32_t voff = (uint32_t)(16 * r * kD * 2 + 16 * n);
-  auto row_at = [&](const char* block, int i) {
+  auto row_at = [&](int P, const char* block, int i) {
+    if constexpr (kNew) {
+      const int t = P * kPair + 16 * r + i;
+      const char* p = t < L0 ? block + voff + i * (kD * 2) : kn + (int64_t)t * src.k_stride + 16 * n;
+      return load_stream(reinterpret_cast<const uint4*>(p));
+    }
     return load_stream(reinterpret_cast<const uint4*>(block + voff + i * (kD * 2)));
   };
   const uint32_t sel4 = (lane & 4) ? 0x03020706u : 0x05040100u;  // byte selectors: 0-3 own, 4-7 the other lane's
@@ -300,7 +357,7 @@ __global__ __launch_bounds__(256, 4) void quantize_kernel(const uint32_t* __rest
   if (base + wave < n_full) {
     const char* const block = K1 + kv.row((base + wave) * kPair) * (kD * 2);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) rows[i] = row_at(block, i);
+    for (int i = 0; i < 16; ++i) rows[i] = row_at(base + wave, block, i);
   }
   float amax[4] = {0.f, 0.f, 0.f, 0.f};
   for (int it = 0; it < bpw; ++it) {
@@ -309,6 +366,12 @@ __global__ __launch_bounds__(256, 4) void quantize_kernel(const uint32_t* __rest
     const bool active = P < n_full;  // the wavefronts of one group are active together
     uint32_t mn[4], mx[4];
     if (active) {
+      if constexpr (kNew) {
+        char* const block = K1 + kv.row(P * kPair) * (kD * 2);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (P * kPair + 16 * r + i >= L0) *reinterpret_cast<uint4*>(block + voff + i * (kD * 2)) = rows[i];
+      }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         rows[i] = make_uint4(P16::prepare(rows[i].x), P16::prepare(rows[i].y), P16::prepare(rows[i].z), P16::prepare(rows[i].w));
@@ -401,7 +464,7 @@ __global__ __launch_bounds__(256, 4) void quantize_kernel(const uint32_t* __rest
       asm volatile("" : "+v"(acc[j]), "+v"(voff));
       if (more) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) rows[4 * j + t] = row_at(block, 4 * j + t);
+        for (int t = 0; t < 4; ++t) rows[4 * j + t] = row_at(P + 4, block, 4 * j + t);
       }
     }
     // even / odd nibbles of tokens 0-7 and 8-15, transposed over the 8 lanes of a channel half
@@ -477,14 +540,14 @@ __global__ __launch_bounds__(256) void append_kernel(uint32_t* __restrict__ K, u
   raise_absmax(kabsmax + (size_t)unit * kD + 2 * lane + 1, gs.amax1());
 }
 
-template <int DT>
-static void launch_quantize_dt(KvLayout lay, const uint32_t* K, uint32_t* kbits, uint32_t* kmeta, float* kabsmax,
+template <int DT, class Rows>
+static void launch_quantize_dt(KvLayout lay, uint32_t* K, uint32_t* kbits, uint32_t* kmeta, float* kabsmax,
                                const int32_t* seq_lens, int units, int n_kv_heads, int max_ctx, int ns, int bpw, int n_x,
-                               hipStream_t st) {
-  const dim3 grid((unsigned)units * (unsigned)(1 + n_x));
+                               int n_copy, Rows src, hipStream_t st) {
+  const dim3 grid((unsigned)units * (unsigned)(1 + n_x + n_copy));
 #define FIER_Q_CASE(NS)                                                                                               \
-  quantize_kernel<DT, NS><<<grid, 256, 0, st>>>(K, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx, bpw, \
-                                                n_x, lay)
+  quantize_kernel<DT, NS, Rows><<<grid, 256, 0, st>>>(K, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx, \
+                                                      bpw, n_x, lay, src)
   switch (ns) {
     case 1: FIER_Q_CASE(1); break;
     case 2: FIER_Q_CASE(2); break;
@@ -511,12 +574,33 @@ hipError_t launch_quantize(int dtype, KvLayout lay, const void* K, uint32_t* kbi
   // apart, and workgroups go round-robin to the 8 XCDs and their CUs: at a multiple of 8 one XCD did everything.  512
   // units of 1000 tokens in 65536 rows: 331 us at n_x = 64, 55 at 65; 128 ragged units up to 64k 279 / 259.
   const int n_x = (n_pairs + 4 * bpw - 1) / (4 * bpw) | 1;
+  uint32_t* const Kw = (uint32_t*)K;  // not written
   if (dtype == DT_F16)
-    launch_quantize_dt<DT_F16>(lay, (const uint32_t*)K, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx, ns,
-                               bpw, n_x, st);
+    launch_quantize_dt<DT_F16>(lay, Kw, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx, ns, bpw, n_x, 0,
+                               CachedRows{}, st);
   else
-    launch_quantize_dt<DT_BF16>(lay, (const uint32_t*)K, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx,
-                                ns, bpw, n_x, st);
+    launch_quantize_dt<DT_BF16>(lay, Kw, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx, ns, bpw, n_x, 0,
+                                CachedRows{}, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_append_chunk(int dtype, KvLayout lay, void* K, uint32_t* kbits, uint32_t* kmeta, float* kabsmax,
+                               const int32_t* seq_lens, NewRows src, int units, int n_kv_heads, int max_ctx, int group_size,
+                               hipStream_t st) {
+  const int ns = group_size / kG;
+  const int span = group_size > kPair ? group_size : kPair;
+  // pair blocks that the longest chunk can touch, wherever it begins in a group
+  const int n_pairs = std::min((src.max_new + span - 2) / span + 1, max_ctx / span) * (span / kPair);
+  src.n_copy = std::min((src.max_new + kPair - 2) / kPair + 1, max_ctx / kPair);
+  const long blocks = (long)n_pairs * units;
+  const int bpw = blocks >= 4L * 4 * 1024 ? 4 : blocks >= 4L * 2 * 1024 ? 2 : 1;  // as in launch_quantize
+  const int n_x = (n_pairs + 4 * bpw - 1) / (4 * bpw) | 1;
+  if (dtype == DT_F16)
+    launch_quantize_dt<DT_F16>(lay, (uint32_t*)K, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx, ns, bpw, n_x,
+                               src.n_copy, src, st);
+  else
+    launch_quantize_dt<DT_BF16>(lay, (uint32_t*)K, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx, ns, bpw, n_x,
+                                src.n_copy, src, st);
   return hipGetLastError();
 }
 

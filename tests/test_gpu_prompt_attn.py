@@ -1,0 +1,260 @@
+"""Causal attention of prompts and of chunks of new tokens over a cache, against the formula in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2508_08256_amd import binding as B
+from prompt_util import D, attention64, check_attention, starts_of, tdtype
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = B.F16, B.BF16
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def i32(a):
+    return torch.as_tensor(np.asarray(a, np.int32), device="cuda")
+
+
+def randn(shape, dtype, seed, scale=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * scale).to(tdtype(dtype))
+
+
+SENTINEL = 7.0
+
+
+def run_prefill(cfg, q, k, v, lens, pad=0, max_new=None, fused=False):
+    n = q.shape[0]
+    fill = lambda t: torch.cat([t, torch.full((pad, *t.shape[1:]), math.nan, dtype=t.dtype)])  # noqa: E731
+    qd, kd, vd = fill(q).cuda(), fill(k).cuda(), fill(v).cuda()
+    if fused:
+        both = torch.cat([qd, kd, vd], dim=1)
+        qd, kd, vd = both.split([q.shape[1], k.shape[1], v.shape[1]], dim=1)
+    out = torch.full((n + pad, q.shape[1], D), SENTINEL, dtype=q.dtype, device="cuda")
+    B.prefill_attn(cfg, qd, kd, vd, i32(starts_of(lens)), max(lens) if max_new is None else max_new, out)
+    torch.cuda.synchronize()
+    return out.cpu()
+
+
+def check_prefill(out, q, k, v, lens, scale):
+    at = 0
+    for b, n in enumerate(lens):
+        if n:
+            want, tol = attention64(q[at:at + n], k[at:at + n], v[at:at + n], 0, scale)
+            check_attention(out[at:at + n], want, tol, f"sequence {b}")
+        at += n
+    assert bool((out[at:] == SENTINEL).all())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("n_q,n_kv", [(1, 1), (4, 4), (8, 4), (3, 1), (8, 2), (10, 2), (6, 1), (7, 1), (16, 2)])
+def test_prompts_of_unequal_lengths(dtype, n_q, n_kv):
+    """Lengths around the tiles of 32 and 64, none, one; every number of heads that share a kv head."""
+    lens = [1, 0, 33, 64, 65, 127, 200]
+    n = sum(lens)
+    cfg = B.make_config(len(lens), n_q, n_kv, 256, dtype)
+    q, k, v = randn((n, n_q, D), dtype, 1), randn((n, n_kv, D), dtype, 2), randn((n, n_kv, D), dtype, 3)
+    for fused in (False, True):
+        check_prefill(run_prefill(cfg, q, k, v, lens, pad=5, fused=fused), q, k, v, lens, cfg.sm_scale)
+
+
+@pytest.mark.parametrize("dtype,n_q,n_kv,n", [(F16, 2, 2, 1500), (BF16, 4, 1, 1025), (F16, 8, 1, 700), (BF16, 1, 1, 2049), (BF16, 32, 32, 300), (F16, 24, 8, 777)])
+def test_long_prompts(dtype, n_q, n_kv, n):
+    cfg = B.make_config(1, n_q, n_kv, 4096, dtype)
+    q, k, v = randn((n, n_q, D), dtype, 4, 1.5), randn((n, n_kv, D), dtype, 5, 1.5), randn((n, n_kv, D), dtype, 6)
+    check_prefill(run_prefill(cfg, q, k, v, [n]), q, k, v, [n], cfg.sm_scale)
+
+
+def test_offsets_that_make_no_sense_stay_inside_the_arrays():
+    """Descending, negative and too large offsets, more tokens than max_new: rows outside are not touched, the first max_new
+    tokens of a sequence are right."""
+    cfg = B.make_config(4, 2, 1, 128, BF16)
+    q, k, v = randn((50, 2, D), BF16, 7), randn((50, 1, D), BF16, 8), randn((50, 1, D), BF16, 9)
+    out = torch.full((50, 2, D), SENTINEL, dtype=torch.bfloat16, device="cuda")
+    B.prefill_attn(cfg, q.cuda(), k.cuda(), v.cuda(), i32([0, 20, -5, 40, 1 << 30]), 12, out)
+    torch.cuda.synchronize()
+    out = out.cpu()
+    for lo in (0, 40):  # 0..19 cut at 12; 20..-5: none; -5..40 begins at 0, cut; 40..50
+        n = min(12, 50 - lo)
+        want, tol = attention64(q[lo:lo + n], k[lo:lo + n], v[lo:lo + n], 0, cfg.sm_scale)
+        check_attention(out[lo:lo + n], want, tol)
+    assert bool((out[12:40] == SENTINEL).all())
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 3e4])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_softmax_scales(dtype, scale):
+    """A negative scale, zero (the mean of V) and one under which the largest logit takes all the weight."""
+    n = 150
+    cfg = B.make_config(1, 4, 2, 256, dtype, sm_scale=scale)
+    q, k, v = randn((n, 4, D), dtype, 10), randn((n, 2, D), dtype, 11), randn((n, 2, D), dtype, 12)
+    if abs(scale) > 1:
+        # the two largest logits of a row must differ by more than binary32 can blur
+        q, k = q.sign() * torch.ones_like(q), k.sign() * torch.ones_like(k)
+        k[torch.arange(n), :, :] = 1
+        q[:] = 1
+        k[:, :, 0] = torch.arange(n, dtype=torch.float32)[:, None].to(k.dtype) - (torch.arange(n) == 40).to(k.dtype)[:, None] * 40
+    got = run_prefill(cfg, q, k, v, [n])
+    if abs(scale) > 1:
+        best = torch.tensor([i - 1 if i == 40 else i for i in range(n)])
+        # One weight p, the others exp2(-4e4) = 0: the result is round(round(p) v / p), each rounding within a factor 1 + u, and
+        # p = 1 only up to the rounding of its logit, so round(p) / p need not be 1.
+        u = torch.finfo(got.dtype).eps / 2
+        for h, kv in ((0, 0), (3, 1)):
+            w = v[best, kv].double()
+            assert bool(((got[:, h].double() - w).abs() <= (2 * u + u * u + 1e-6) * w.abs() + 2.0**-25).all())
+    else:
+        check_prefill(got, q, k, v, [n], cfg.sm_scale)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_logits_far_beyond_24_bits(dtype):
+    """Equal rows under huge logits: the mean of V.  (Weights must not move with the rounding of the largest logit.)"""
+    n, big = 90, (250.0 if dtype == F16 else 1e15)
+    cfg = B.make_config(1, 2, 1, 128, dtype, sm_scale=1e3)
+    q = torch.full((n, 2, D), big).to(tdtype(dtype))
+    k = torch.full((n, 1, D), big).to(tdtype(dtype))
+    v = randn((n, 1, D), dtype, 13)
+    got = run_prefill(cfg, q, k, v, [n])
+    mean = v[:, 0].double().cumsum(0) / torch.arange(1, n + 1)[:, None]
+    size = v[:, 0].double().abs().cumsum(0) / torch.arange(1, n + 1)[:, None]
+    u = torch.finfo(tdtype(dtype)).eps / 2
+    assert bool(((got[:, 0].double() - mean).abs() <= u * mean.abs() + (u + 1e-5) * size + 1e-7).all())
+
+
+def make_cache(cfg, first, new, dtype, block_tokens, seed):
+    """Rows [0, first + new) of every sequence random, everything else NaN; K, V per sequence on the host too."""
+    cap, nb, hkv = cfg.max_ctx, cfg.batch, cfg.n_kv_heads
+    rows = []
+    for which in (0, 1):
+        t = torch.full((nb, hkv, cap, D), math.nan, dtype=tdtype(dtype))
+        for b in range(nb):
+            n = min(cap, first[b] + new[b])
+            t[b, :, :n] = randn((hkv, n, D), dtype, seed + 10 * b + which)
+        rows.append(t)
+    table = None
+    dev = [t.view(nb * hkv, cap, D).cuda() for t in rows]
+    if block_tokens:
+        per = cap // block_tokens
+        perm = torch.randperm(nb * per + 3, generator=torch.Generator().manual_seed(seed))
+        table = perm[: nb * per].view(nb, per).to(torch.int32)
+        pools = []
+        for t in rows:
+            pool = torch.full((nb * per + 3, hkv, block_tokens, D), math.nan, dtype=t.dtype)
+            pool[table.long()] = t.view(nb, hkv, per, block_tokens, D).transpose(1, 2)
+            pools.append(pool.cuda())
+        dev, table = pools, table.cuda()
+    return rows, B.DeviceCache(cfg, dev[0], dev[1], i32(first), table)
+
+
+def run_chunk(cfg, cache, q, new, pad=0, ws=None, max_new=None):
+    qd = torch.cat([q, torch.full((pad, *q.shape[1:]), math.nan, dtype=q.dtype)]).cuda()
+    out = torch.full(qd.shape, SENTINEL, dtype=q.dtype, device="cuda")
+    max_new = max(max(new), 1) if max_new is None else max_new
+    ws = B.make_chunk_workspace(cfg, qd.shape[0], max_new) if ws is None else ws
+    B.chunk_attn(cfg, cache, qd, i32(starts_of(new)), max_new, out, ws)
+    torch.cuda.synchronize()
+    return out.cpu()
+
+
+def check_chunk(out, q, rows, first, new, cfg):
+    at = 0
+    for b, n in enumerate(new):
+        if n:
+            k, v = (t[b].transpose(0, 1) for t in rows)
+            want, tol = attention64(q[at:at + n], k, v, first[b], cfg.sm_scale, cap=cfg.max_ctx)
+            check_attention(out[at:at + n], want, tol, f"sequence {b}")
+        at += n
+    assert bool((out[at:] == SENTINEL).all())
+
+
+@pytest.mark.parametrize("block_tokens", [0, 64, 256])
+@pytest.mark.parametrize("dtype,n_q,n_kv", [(F16, 4, 4), (BF16, 8, 2), (BF16, 6, 2), (F16, 8, 1), (BF16, 5, 1), (F16, 14, 2)])
+def test_chunks_of_unequal_lengths(dtype, n_q, n_kv, block_tokens):
+    first = [0, 63, 64, 500, 1000, 127, 1]
+    new = [70, 1, 0, 33, 9, 130, 64]
+    cfg = B.make_config(len(first), n_q, n_kv, 1280, dtype)
+    rows, cache = make_cache(cfg, first, new, dtype, block_tokens, 20)
+    q = randn((sum(new), n_q, D), dtype, 21)
+    check_chunk(run_chunk(cfg, cache, q, new, pad=3), q, rows, first, new, cfg)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("n_q,n_kv", [(1, 1), (2, 1), (8, 1), (8, 8), (12, 4)])
+@pytest.mark.parametrize("new", [1, 2, 5])
+def test_single_and_drafted_tokens_over_long_caches(dtype, n_q, n_kv, new):
+    """Few rows: the caches are split over many workgroups.  Lengths from an empty cache to 9000, blocks that end anywhere."""
+    first = [0, 31, 2047, 9000]
+    cfg = B.make_config(4, n_q, n_kv, 9216, dtype)
+    rows, cache = make_cache(cfg, first, [new] * 4, dtype, 64 if new == 2 else 0, 30 + new)
+    q = randn((4 * new, n_q, D), dtype, 31)
+    ws = B.make_chunk_workspace(cfg, 4 * new, new)
+    for _ in range(3):  # the workspace is left ready for the next call
+        check_chunk(run_chunk(cfg, cache, q, [new] * 4, ws=ws), q, rows, first, [new] * 4, cfg)
+
+
+@pytest.mark.parametrize("dtype,n_q,n_kv,first,new", [(BF16, 8, 2, 5000, 300), (F16, 4, 4, 3001, 129), (BF16, 1, 1, 20000, 40), (F16, 16, 2, 700, 600)])
+def test_long_chunks_behind_long_contexts(dtype, n_q, n_kv, first, new):
+    cap = -(-(first + new) // 64) * 64
+    cfg = B.make_config(1, n_q, n_kv, cap, dtype)
+    rows, cache = make_cache(cfg, [first], [new], dtype, 64, 40)
+    q = randn((new, n_q, D), dtype, 41)
+    check_chunk(run_chunk(cfg, cache, q, [new]), q, rows, [first], [new], cfg)
+
+
+def test_a_full_cache():
+    """Tokens past the capacity attend over all of its rows; lengths above it count as full, below 0 as empty."""
+    cfg = B.make_config(3, 4, 2, 256, BF16)
+    first, new = [250, 256, 0], [20, 3, 2]
+    rows, cache = make_cache(cfg, first, new, BF16, 64, 50)
+    cache.seq_lens.copy_(i32([250, 300, -4]))
+    q = randn((25, 4, D), BF16, 51)
+    check_chunk(run_chunk(cfg, cache, q, new), q, rows, first, new, cfg)
+
+
+def test_chunks_on_another_stream_and_in_a_graph():
+    """Captured with two workspaces in one graph, replayed with eager work on the first in between: the eager result."""
+    cfg = B.make_config(2, 8, 2, 4096, BF16)
+    first, new = [4000, 1200], [4, 2]
+    rows, cache = make_cache(cfg, first, new, BF16, 64, 60)
+    q = randn((6, 8, D), BF16, 61)
+    want = run_chunk(cfg, cache, q, new)
+    check_chunk(want, q, rows, first, new, cfg)
+    qd, starts = q.cuda(), i32(starts_of(new))
+    ws = [B.make_chunk_workspace(cfg, 6, 4) for _ in range(2)]
+    outs = [torch.zeros(6, 8, D, dtype=q.dtype, device="cuda") for _ in range(3)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        B.chunk_attn(cfg, cache, qd, starts, 4, outs[2], ws[0])
+    side.synchronize()
+    assert torch.equal(outs[2].cpu(), want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for o, w in zip(outs, ws):
+            B.chunk_attn(cfg, cache, qd, starts, 4, o, w)
+    for _ in range(4):
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0].cpu(), want) and torch.equal(outs[1].cpu(), want)
+        B.chunk_attn(cfg, cache, qd, starts, 4, outs[2], ws[0])
+        torch.cuda.synchronize()
+        assert torch.equal(outs[2].cpu(), want)
+
+
+def test_results_do_not_change_from_call_to_call():
+    cfg = B.make_config(2, 8, 8, 2048, F16)
+    rows, cache = make_cache(cfg, [2000, 700], [3, 1], F16, 0, 70)
+    q = randn((4, 8, D), F16, 71)
+    ws = B.make_chunk_workspace(cfg, 4, 3)
+    ref = run_chunk(cfg, cache, q, [3, 1], ws=ws)
+    for _ in range(10):
+        assert torch.equal(run_chunk(cfg, cache, q, [3, 1], ws=ws), ref)
