@@ -591,7 +591,7 @@ int fier_decode_step_static(const fier_config* cfg, const fier_cache* layers, in
 // ---- many new tokens per sequence -----------------------------------------------------------------------------------
 // q, k, v rows as the caller's projections left them: `stride` elements from a token to the next, its heads side by side.
 static int check_rows(const void* p, int64_t stride, int heads) {
-  if (stride < (int64_t)heads * kD || stride > (int64_t)1 << 40) return FIER_ESHAPE;
+  if (stride < (int64_t)heads * kD || stride > 1 << 24) return FIER_ESHAPE;  // a tile's offsets fit 32 bits
   return misaligned(p) || stride % 8 != 0 ? FIER_EALIGN : FIER_OK;
 }
 constexpr int32_t kMaxNewTokens = 1 << 24;  // rows of the new tokens: query rows of a unit then fit 32 bits
@@ -621,6 +621,9 @@ static fier::PromptArgs prompt_args(const fier_config* cfg, const void* q, int64
   a.n_tokens = n_tokens;
   a.max_new = std::min(max_new, n_tokens);
   a.kv_cap = INT32_MAX;
+  const fier::PromptSplit sp = fier::prompt_split(a.units, a.n_rep, a.max_new, 0);
+  a.row_tiles = sp.row_tiles;
+  a.side_parts = a.shared_parts = 1;
   return a;
 }
 
@@ -659,12 +662,19 @@ int fier_chunk_attn(const fier_config* cfg, const fier_cache* cache, const void*
   a.lay = layout_of(cfg, cache);
   a.kv_cap = cfg->max_ctx;
   a.from_cache = true;
+  const fier::PromptSplit sp = fier::prompt_split(a.units, a.n_rep, a.max_new, a.kv_cap);
+  a.side_parts = sp.side_parts, a.shared_parts = sp.shared_parts;
+  const Workspace w = carve(cfg, 1, workspace);
+  a.counters = w.sb.hist;
+  a.side_partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.zero_bytes);
+  a.shared_partials = a.side_partials + sp.side_floats;
   return fier::launch_prompt_attn(cfg->kv_dtype, a, (hipStream_t)stream);
 }
 
 size_t fier_chunk_workspace_bytes(const fier_config* cfg, int32_t n_tokens, int32_t max_new) {
   if (check_cfg(cfg) != FIER_OK || n_tokens < 0 || n_tokens > kMaxNewTokens || max_new < 0) return 0;
-  return carve(cfg, 1, nullptr).zero_bytes;
+  const fier::PromptSplit sp = fier::prompt_split(units_of(cfg), n_rep_of(cfg), std::min(max_new, n_tokens), cfg->max_ctx);
+  return carve(cfg, 1, nullptr).zero_bytes + align_up((sp.side_floats + sp.shared_floats) * sizeof(float));
 }
 
 int fier_append_chunk(const fier_config* cfg, const fier_cache* cache, const void* k_new, int64_t k_stride,
