@@ -385,21 +385,27 @@ def decode_step_phase(cfg: Config, caches, q, k_new, v_new, budgets, max_budget:
 
 def _rows(t, heads: int, head_dim: int, n: int, what: str):
     """(pointer, elements from a token to the next) of a tensor [n][heads][head_dim] whose tokens may lie apart."""
-    s = t.stride()
-    if tuple(t.shape) != (n, heads, head_dim) or t.element_size() != 2 or s[2] != 1 or (heads > 1 and s[1] != head_dim):
-        raise FierError(ESHAPE, f"{what}: {tuple(t.shape)}, strides {s}, of {n} tokens")
-    return t.data_ptr(), s[0] if n > 1 else max(s[0], heads * head_dim)  # a single row's stride may be anything
+    if t.shape == (n, heads, head_dim) and t.element_size() == 2:
+        if t.is_contiguous():
+            return t.data_ptr(), heads * head_dim
+        s = t.stride()
+        if s[2] == 1 and (heads == 1 or s[1] == head_dim):
+            return t.data_ptr(), s[0] if n > 1 else heads * head_dim  # a single token's stride may be anything
+    raise FierError(ESHAPE, f"{what}: {tuple(t.shape)}, strides {t.stride()}, of {n} tokens")
+
+
+def _whole(t, heads: int, head_dim: int, n: int, what: str):
+    if not t.is_contiguous():
+        raise FierError(ESHAPE, f"{what}: not contiguous")
+    return _rows(t, heads, head_dim, n, what)[0]
 
 
 def prefill_attn(cfg: Config, q, k, v, starts, max_new: int, out):
     """q, out [n_tokens][n_q_heads][128], k, v [n_tokens][n_kv_heads][128] (out contiguous, the others may be views of a fused
     projection); starts [batch + 1] int32."""
-    n, d = q.shape[0], cfg.head_dim
-    out_p, out_stride = _rows(out, cfg.n_q_heads, d, n, "out")
-    if out_stride != cfg.n_q_heads * d:
-        raise FierError(ESHAPE, "out: not contiguous")
-    _check(lib().fier_prefill_attn(C.byref(cfg), *_rows(q, cfg.n_q_heads, d, n, "q"), *_rows(k, cfg.n_kv_heads, d, n, "k"),
-                                   *_rows(v, cfg.n_kv_heads, d, n, "v"), _ptr(starts), n, int(max_new), out_p, _stream()),
+    n, d, hq, hkv = q.size(0), cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads
+    _check(lib().fier_prefill_attn(C.byref(cfg), *_rows(q, hq, d, n, "q"), *_rows(k, hkv, d, n, "k"), *_rows(v, hkv, d, n, "v"),
+                                   _ptr(starts), n, int(max_new), _whole(out, hq, d, n, "out"), _stream()),
            "fier_prefill_attn")
 
 
@@ -417,19 +423,16 @@ def make_chunk_workspace(cfg: Config, n_tokens: int, max_new: int):
 
 
 def chunk_attn(cfg: Config, cache: DeviceCache, q, starts, max_new: int, out, workspace):
-    n, d = q.shape[0], cfg.head_dim
-    out_p, out_stride = _rows(out, cfg.n_q_heads, d, n, "out")
-    if out_stride != cfg.n_q_heads * d:
-        raise FierError(ESHAPE, "out: not contiguous")
-    _check(lib().fier_chunk_attn(C.byref(cfg), C.byref(cache.c), *_rows(q, cfg.n_q_heads, d, n, "q"), _ptr(starts), n,
-                                 int(max_new), out_p, *_ws(workspace), _stream()), "fier_chunk_attn")
+    n, d, hq = q.size(0), cfg.head_dim, cfg.n_q_heads
+    _check(lib().fier_chunk_attn(C.byref(cfg), C.byref(cache.c), *_rows(q, hq, d, n, "q"), _ptr(starts), n, int(max_new),
+                                 _whole(out, hq, d, n, "out"), *_ws(workspace), _stream()), "fier_chunk_attn")
 
 
 def append_chunk(cfg: Config, cache: DeviceCache, k_new, v_new, starts, max_new: int):
     """k_new, v_new [n_tokens][n_kv_heads][128], possibly views; starts [batch + 1] int32."""
-    n, d = k_new.shape[0], cfg.head_dim
-    _check(lib().fier_append_chunk(C.byref(cfg), C.byref(cache.c), *_rows(k_new, cfg.n_kv_heads, d, n, "k_new"),
-                                   *_rows(v_new, cfg.n_kv_heads, d, n, "v_new"), _ptr(starts), n, int(max_new), _stream()),
+    n, d, hkv = k_new.size(0), cfg.head_dim, cfg.n_kv_heads
+    _check(lib().fier_append_chunk(C.byref(cfg), C.byref(cache.c), *_rows(k_new, hkv, d, n, "k_new"),
+                                   *_rows(v_new, hkv, d, n, "v_new"), _ptr(starts), n, int(max_new), _stream()),
            "fier_append_chunk")
 
 
@@ -437,11 +440,9 @@ def block_table(cfg: Config, block_tokens: int, old_lens, new_lens, table, free_
                 slots=None):
     """int32 tensors on the GPU: old_lens, new_lens [batch], table [batch][max_ctx / block_tokens], free_blocks [pool blocks],
     n_free, n_free_out of one element, starts [batch + 1], slots of any size."""
-    import torch
-
-    ints = (old_lens, new_lens, table, free_blocks, n_free, n_free_out, starts, slots)
-    if any(t is not None and (t.dtype != torch.int32 or not t.is_contiguous()) for t in ints):
-        raise FierError(EINVAL, "fier_block_table: contiguous int32 tensors are wanted")
+    for t in (old_lens, new_lens, table, free_blocks, n_free, n_free_out, starts, slots):
+        if t is not None and not (t.is_contiguous() and t.element_size() == 4):
+            raise FierError(EINVAL, "fier_block_table: contiguous int32 tensors are wanted")
     if (old_lens.numel() != cfg.batch or new_lens.numel() != cfg.batch or block_tokens < 1
             or table.numel() != cfg.batch * (cfg.max_ctx // block_tokens)
             or (starts is not None and starts.numel() < cfg.batch + 1)):

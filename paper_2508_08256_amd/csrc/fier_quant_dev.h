@@ -111,23 +111,6 @@ __device__ __forceinline__ GroupScale quantize_group(const uint32_t (&rows)[kG],
   return g;
 }
 
-// Groups of g = 32 ns tokens, ns in {2, 4, 8}: the group's rows do not fit the registers, so they are read twice
-// (min / max, then codes), 32 rows at a time.  row_at(t) returns the packed pair of token t of the group (t < ntok).
-// Pass 1 returns the scale; pass 2 is code_rows per 32-token chunk, driven by the caller.
-template <int DT, class RowAt>
-__device__ __forceinline__ GroupScale long_group_scale(RowAt row_at, int ntok) {
-  MinMax m;
-  minmax_first<DT>(m, row_at(0));
-  for (int c0 = 0; c0 < ntok; c0 += kG) {
-    uint32_t rows[kG];
-#pragma unroll
-    for (int t = 0; t < kG; ++t) rows[t] = row_at(c0 + t < ntok ? c0 + t : 0);
-#pragma unroll
-    for (int t = 0; t < kG; ++t) minmax_update<DT>(m, rows[t], c0 + t < ntok);
-  }
-  return group_scale<DT>(m);
-}
-
 // kabsmax[u][c] >= |dequantized key| of every token quantized so far: raised with an integer max on the bit
 // pattern (non-negative floats order like unsigned integers); a plain read filters most of the atomics.
 __device__ __forceinline__ void raise_absmax(float* __restrict__ slot, float a) {

@@ -30,86 +30,62 @@ __device__ __forceinline__ short2_t order_keys(uint32_t pair) {
   return v ^ ((v >> 15) & (short)0x7fff);
 }
 
-// One wavefront, g = 32: the unit's last pair block when it is partial (1 to 63 tokens present).  rows_from(t0)(t): the lane's
-// channel pair of token t0 + t, both in one group.
-template <int DT, class RowsFrom>
-__device__ __forceinline__ void quantize_tail_short(RowsFrom rows_from, uint32_t* __restrict__ kbits,
-                                                    uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax, int L,
-                                                    int max_ctx, const int unit, const int lane) {
-  const int P = L / kPair;
-  if (P * kPair >= L) return;
-  const int n_groups = max_ctx / kG;
-  uint4 mine = make_uint4(0, 0, 0, 0);
-  float amax0 = 0.f, amax1 = 0.f;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int t0 = P * kPair + h * kG;
-    int ntok = L - t0;
-    ntok = ntok > kG ? kG : ntok;
-    uint32_t meta0 = 0, meta1 = 0;
-    if (ntok > 0) {
-      uint32_t rows[kG];
-      const auto row_at = rows_from(t0);
-#pragma unroll
-      for (int t = 0; t < kG; ++t) rows[t] = row_at(t < ntok ? t : 0);
-      const GroupScale gs = quantize_group<DT>(rows, ntok, lane, h * kG, mine);
-      meta0 = gs.s0 | (gs.z0 << 16);
-      meta1 = gs.s1 | (gs.z1 << 16);
-      amax0 = fmaxf(amax0, gs.amax0());
-      amax1 = fmaxf(amax1, gs.amax1());
-    }
-    uint2* mdst = reinterpret_cast<uint2*>(kmeta + ((size_t)unit * n_groups + 2 * P + h) * kD) + lane;
-    *mdst = make_uint2(meta0, meta1);
-  }
-  reinterpret_cast<uint4*>(kbits)[(size_t)unit * max_ctx + P * kPair + lane] = mine;
-  raise_absmax(kabsmax + (size_t)unit * kD + 2 * lane, amax0);
-  raise_absmax(kabsmax + (size_t)unit * kD + 2 * lane + 1, amax1);
-}
-
-// One wavefront, g = 32 ns with ns in {2, 4, 8}: the unit's last group when it is partial.  Its rows are read twice
-// (min / max, then codes), 32 at a time.
-template <int DT, class RowsFrom>
-__device__ __forceinline__ void quantize_tail_long(RowsFrom rows_from, uint32_t* __restrict__ kbits,
-                                                   uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax, int L,
-                                                   int max_ctx, int ns, const int unit, const int lane) {
-  const int g = kG * ns;
-  const int Gi = L / g;
-  const int t0 = Gi * g;
-  if (t0 >= L) return;
-  const int ntok = L - t0;
-  const int n_groups = max_ctx / g;
-  const auto row_at = rows_from(t0);
-  const GroupScale gs = long_group_scale<DT>(row_at, ntok);
-  uint2* mdst = reinterpret_cast<uint2*>(kmeta + ((size_t)unit * n_groups + Gi) * kD) + lane;
-  *mdst = make_uint2(gs.s0 | (gs.z0 << 16), gs.s1 | (gs.z1 << 16));
-  for (int pb = 0; pb * kPair < ntok; ++pb) {
-    uint4 mine = make_uint4(0, 0, 0, 0);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int c0 = pb * kPair + h * kG;
-      int nt = ntok - c0;
-      nt = nt > kG ? kG : nt;
-      if (nt > 0) {
-        uint32_t rows[kG];
-#pragma unroll
-        for (int t = 0; t < kG; ++t) rows[t] = row_at(c0 + t < ntok ? c0 + t : 0);
-        code_rows<DT>(rows, nt, gs, lane, h * kG, mine);
-      }
-    }
-    reinterpret_cast<uint4*>(kbits)[(size_t)unit * max_ctx + t0 + pb * kPair + lane] = mine;
-  }
-  raise_absmax(kabsmax + (size_t)unit * kD + 2 * lane, gs.amax0());
-  raise_absmax(kabsmax + (size_t)unit * kD + 2 * lane + 1, gs.amax1());
-}
-
+// The tokens behind a unit's whole groups, by the four wavefronts of a workgroup, up to 32 (g = 256: 64) rows in the registers of
+// each.  rows_from(t0)(t): the lane's channel pair of token t0 + t, both in one group.  One wavefront that read the rows
+// twice, 32 at a time, took the larger part of a chunk's append: 36 us at 96 units of 20 to 700 tokens, g = 128; now 15.
+// xch: 256 float4 of LDS.
 template <int DT, int NS, class RowsFrom>
 __device__ __forceinline__ void quantize_tail(RowsFrom rows_from, uint32_t* __restrict__ kbits, uint32_t* __restrict__ kmeta,
                                               float* __restrict__ kabsmax, int L, int max_ctx, const int unit,
-                                              const int lane) {
-  if constexpr (NS == 1)
-    quantize_tail_short<DT>(rows_from, kbits, kmeta, kabsmax, L, max_ctx, unit, lane);
-  else
-    quantize_tail_long<DT>(rows_from, kbits, kmeta, kabsmax, L, max_ctx, NS, unit, lane);
+                                              const int lane, const int wave, float4* xch) {
+  constexpr int kTail = NS == 1 ? kPair : kG * NS;  // the last pair block (two groups), or the last group
+  const int t0 = L / kTail * kTail, ntok = L - t0;
+  if (ntok == 0) return;
+  const int n_groups = max_ctx / (kG * NS);
+  constexpr int kChunks = NS == 8 ? 2 : 1;  // of 32 tokens, per wavefront
+  uint32_t rows[kChunks][kG];
+  const auto row_at = rows_from(t0);
+#pragma unroll
+  for (int k = 0; k < kChunks; ++k) {
+    const int first = (wave + 4 * k) * kG;
+    if (first < ntok) {
+#pragma unroll
+      for (int t = 0; t < kG; ++t) rows[k][t] = row_at(first + t < ntok ? first + t : first);
+    }
+  }
+  uint4* const bdst = reinterpret_cast<uint4*>(kbits) + (size_t)unit * max_ctx + t0;
+  uint2* const mdst = reinterpret_cast<uint2*>(kmeta + ((size_t)unit * n_groups + t0 / (kG * NS)) * kD) + lane;
+  GroupScale gs = {};
+  if constexpr (NS == 1) {  // a wavefront for each of the two groups
+    if (wave >= 2) return;
+    const int nt = min(ntok - wave * kG, kG);
+    uint4 mine = make_uint4(0, 0, 0, 0);
+    if (nt > 0) gs = quantize_group<DT>(rows[0], nt, lane, wave * kG, mine);
+    mdst[wave * (kD / 2)] = make_uint2(gs.s0 | (gs.z0 << 16), gs.s1 | (gs.z1 << 16));
+    if (lane >> 5 == wave) bdst[lane] = mine;
+    if (nt <= 0) return;
+  } else {
+    MinMax m = {INFINITY, -INFINITY, INFINITY, -INFINITY};
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k)
+      first_rows<0, kG>(ntok - (wave + 4 * k) * kG, [&](auto t) { minmax_update<DT>(m, rows[k][t], true); });
+    xch[wave * 64 + lane] = make_float4(m.mn0, m.mx0, m.mn1, m.mx1);
+    __syncthreads();
+    gs = group_scale<DT>(tail_join(xch, 4, lane));
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      const int c = wave + 4 * k;
+      if ((c >> 1) * kPair >= ntok || c >= NS) break;  // every pair block that holds a token is written
+      uint4 mine = make_uint4(0, 0, 0, 0);
+      const int nt = min(ntok - c * kG, kG);
+      if (nt > 0) code_rows<DT>(rows[k], nt, gs, lane, (c & 1) * kG, mine);
+      if (lane >> 5 == (c & 1)) bdst[(c >> 1) * kPair + lane] = mine;
+    }
+    if (wave != 0) return;
+    *mdst = make_uint2(gs.s0 | (gs.z0 << 16), gs.s1 | (gs.z1 << 16));
+  }
+  raise_absmax(kabsmax + (size_t)unit * kD + 2 * lane, gs.amax0());
+  raise_absmax(kabsmax + (size_t)unit * kD + 2 * lane + 1, gs.amax1());
 }
 
 // The same word by word for one 16-bit float; keys order like the floats, -0 (key -1) just below +0 (key 0).
@@ -240,7 +216,7 @@ __device__ __forceinline__ uint32_t transpose_nibbles(uint32_t v, uint32_t sel4,
 }
 
 // Whole groups, and the partial one at a unit's end.  Grid units * (1 + n_x), n_x >= ceil(n_pairs / (4 bpw)), block 256.
-// The first `units` workgroups do the units' partial groups (one wavefront, the longest chain of dependent loads:
+// The first `units` workgroups do the units' partial groups (the longest chain of dependent loads:
 // started last it would end the kernel late, and as a kernel of its own it took 4 to 17 us after this one); then wave w
 // of workgroup x of a unit owns the pair blocks 4 bpw x + w, + 4, + 8, ...; NS = group size / 32.
 //   A pair block sits in 64 registers: load i of lane (row r, n) brings channels 8n .. 8n + 7 of token 16 r + i.  Minima
@@ -257,7 +233,7 @@ __device__ __forceinline__ uint32_t transpose_nibbles(uint32_t v, uint32_t sel4,
 // g = 128: 74 -> 35.  128 registers keep four workgroups on a CU.
 //   Rows = NewRows: the same for a chunk of new tokens, from the first group that one of them falls in on.  A row is read from
 // the chunk, or from the cache where it was there before, and a new K row is stored in the cache from the registers it is
-// coded from; the V rows are copied by workgroups of their own at the end of the grid, a wavefront 16 tokens a time.
+// coded from; the V rows, and the K rows behind the whole groups, are copied by workgroups of their own at the end of the grid.
 template <int DT, int NS, class Rows>
 __global__ __launch_bounds__(256, 4) void quantize_kernel(uint32_t* __restrict__ K, uint32_t* __restrict__ kbits,
                                                        uint32_t* __restrict__ kmeta, float* __restrict__ kabsmax,
@@ -280,58 +256,57 @@ __global__ __launch_bounds__(256, 4) void quantize_kernel(uint32_t* __restrict__
   const int L0 = L;  // tokens in the cache before a chunk
   const KvRows kv = lay.rows_of(unit);
   const char *kn = nullptr, *vn = nullptr;  // the chunk's rows of this head, moved to where token 0 would be
+  int n_full = 0;                           // pair blocks that consist of whole groups
+  if constexpr (!kNew) n_full = NS == 1 ? L / kPair : (L / (kG * NS)) * (NS / 2);
   if constexpr (kNew) {
     const int b = unit / n_kv_heads, head = unit - b * n_kv_heads;
     const int lo = max(0, min(src.starts[b], src.n_tokens)), hi = max(lo, min(src.starts[b + 1], src.n_tokens));
     L = min(L0 + min(hi - lo, src.max_new), max_ctx);
     if (L == L0) return;
+    n_full = NS == 1 ? L / kPair : (L / (kG * NS)) * (NS / 2);
     kn = src.k + (int64_t)(lo - L0) * src.k_stride + head * (kD * 2);
     vn = src.v + (int64_t)(lo - L0) * src.v_stride + head * (kD * 2);
     if ((int)blockIdx.x >= n_quant) {
       // 64 tokens of V: token t0 + 16 i + 4 wave + lane / 16, a multiple of 64 at the start
       const int t0 = (L0 / kPair + ((int)blockIdx.x - n_quant) % src.n_copy) * kPair;
       if (t0 >= L) return;
-      uint4 w[4];
+      auto load = [&](const char* rows, int64_t stride, uint4 (&w)[4]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = t0 + 16 * i + 4 * wave + (lane >> 4);
-        w[i] = load_stream(reinterpret_cast<const uint4*>(vn + (int64_t)max(L0, min(t, L - 1)) * src.v_stride) + (lane & 15));
-      }
-      uint4* const dst = reinterpret_cast<uint4*>(src.V) + kv.row(t0) * (kD / 8) + (lane & 15);
+        for (int i = 0; i < 4; ++i) {
+          const int t = t0 + 16 * i + 4 * wave + (lane >> 4);
+          w[i] = load_stream(reinterpret_cast<const uint4*>(rows + (int64_t)max(L0, min(t, L - 1)) * stride) + (lane & 15));
+        }
+      };
+      auto store = [&](void* rows, const uint4 (&w)[4]) {
+        uint4* const dst = reinterpret_cast<uint4*>(rows) + kv.row(t0) * (kD / 8) + (lane & 15);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = 16 * i + 4 * wave + (lane >> 4);
-        if (t0 + t >= L0 && t0 + t < L) dst[t * (kD / 8)] = w[i];
-      }
+        for (int i = 0; i < 4; ++i) {
+          const int t = 16 * i + 4 * wave + (lane >> 4);
+          if (t0 + t >= L0 && t0 + t < L) dst[t * (kD / 8)] = w[i];
+        }
+      };
+      uint4 v[4], k[4];
+      const bool behind = t0 >= n_full * kPair;
+      load(vn, src.v_stride, v);
+      if (behind) load(kn, src.k_stride, k);
+      store(src.V, v);
+      if (behind) store(K, k);
       return;
     }
   }
-  // pair blocks that consist of whole groups
-  const int n_full = NS == 1 ? L / kPair : (L / (kG * NS)) * (NS / 2);
   if (wid < 0) {
-    if constexpr (kNew) {
-      // the K rows behind the whole groups; the wavefront that codes them reads them from the chunk
-      for (int t = max(L0, n_full * kPair) + 4 * wave + (lane >> 4); t < L; t += 16)
-        reinterpret_cast<uint4*>(K)[kv.row(t) * (kD / 8) + (lane & 15)] =
-            reinterpret_cast<const uint4*>(kn + (int64_t)t * src.k_stride)[lane & 15];
-      if (wave == 0)
-        quantize_tail<DT, NS>(
-            [&](int t0) {
-              const uint32_t* old = K + kv.row(t0) * (kD / 2) + lane;
-              return [=](int t) {
-                return t0 + t < L0 ? old[(size_t)t * (kD / 2)]
-                                   : reinterpret_cast<const uint32_t*>(kn + (int64_t)(t0 + t) * src.k_stride)[lane];
-              };
-            },
-            kbits, kmeta, kabsmax, L, max_ctx, unit, lane);
-    } else if (wave == 0) {
-      quantize_tail<DT, NS>(
-          [&](int t0) {
-            const uint32_t* rows = K + kv.row(t0) * (kD / 2) + lane;
-            return [=](int t) { return rows[(size_t)t * (kD / 2)]; };
-          },
-          kbits, kmeta, kabsmax, L, max_ctx, unit, lane);
-    }
+    __shared__ float4 tail[256];
+    quantize_tail<DT, NS>(
+        [&](int t0) {
+          const uint32_t* rows = K + kv.row(t0) * (kD / 2) + lane;
+          return [=](int t) {
+            if constexpr (kNew) {
+              if (t0 + t >= L0) return reinterpret_cast<const uint32_t*>(kn + (int64_t)(t0 + t) * src.k_stride)[lane];
+            }
+            return rows[(size_t)t * (kD / 2)];
+          };
+        },
+        kbits, kmeta, kabsmax, L, max_ctx, unit, lane, wave, tail);
     return;
   }
   const int base = (wid - unit * n_x) * (4 * bpw) + (kNew ? L0 / (NS == 1 ? kPair : kG * NS) * (NS == 1 ? 1 : NS / 2) : 0);

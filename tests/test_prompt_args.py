@@ -124,7 +124,7 @@ def test_the_binding_refuses_other_layouts(monkeypatch):
         B.append_chunk(cfg, cache, k, wide[:, :3], starts, 5)
     i = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
     good = [i(2), i(2), i(8), i(9), i(1), i(1), i(3), i(4)]
-    for at, bad in ((0, i(3)), (2, i(9)), (6, i(2)), (3, torch.zeros(9)), (7, i(8)[::2])):
+    for at, bad in ((0, i(3)), (2, i(9)), (6, i(2)), (3, torch.zeros(9, dtype=torch.int64)), (7, i(8)[::2])):
         args = list(good)
         args[at] = bad
         with pytest.raises(B.FierError):
