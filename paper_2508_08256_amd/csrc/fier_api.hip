@@ -614,17 +614,18 @@ static fier::PromptArgs prompt_args(const fier_config* cfg, const void* q, int64
   a.scale = cfg->sm_scale == 0.f ? 1.f : std::fabs(cfg->sm_scale) * 1.4426950408889634f;
   a.flip = cfg->sm_scale < 0.f ? 0x80008000u : 0u;
   a.keep = cfg->sm_scale == 0.f ? 0u : 0xffffffffu;
-  a.units = units_of(cfg);
+  a.batch = cfg->batch;
   a.n_kv_heads = cfg->n_kv_heads;
   a.n_q_heads = cfg->n_q_heads;
   a.n_rep = n_rep_of(cfg);
   a.n_tokens = n_tokens;
   a.max_new = std::min(max_new, n_tokens);
   a.kv_cap = INT32_MAX;
-  const fier::PromptSplit sp = fier::prompt_split(a.units, a.n_rep, a.max_new, 0);
-  a.row_tiles = sp.row_tiles;
-  a.side_parts = a.shared_parts = 1;
   return a;
+}
+// split: with a workspace for partial results
+static fier::PromptSplit prompt_split(const fier_config* cfg, int32_t n_tokens, int32_t max_new, bool split) {
+  return fier::prompt_split(cfg->batch, cfg->n_kv_heads, n_rep_of(cfg), n_tokens, std::min(max_new, n_tokens), split);
 }
 
 int fier_prefill_attn(const fier_config* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
@@ -640,7 +641,7 @@ int fier_prefill_attn(const fier_config* cfg, const void* q, int64_t q_stride, c
   fier::PromptArgs a = prompt_args(cfg, q, q_stride, starts, n_tokens, max_new, out);
   a.k = static_cast<const char*>(k), a.v = static_cast<const char*>(v);
   a.k_stride = 2 * k_stride, a.v_stride = 2 * v_stride;
-  return fier::launch_prompt_attn(cfg->kv_dtype, a, (hipStream_t)stream);
+  return fier::launch_prompt_attn(cfg->kv_dtype, a, prompt_split(cfg, n_tokens, max_new, false), (hipStream_t)stream);
 }
 
 int fier_chunk_attn(const fier_config* cfg, const fier_cache* cache, const void* q, int64_t q_stride, const int32_t* starts,
@@ -662,18 +663,15 @@ int fier_chunk_attn(const fier_config* cfg, const fier_cache* cache, const void*
   a.lay = layout_of(cfg, cache);
   a.kv_cap = cfg->max_ctx;
   a.from_cache = true;
-  const fier::PromptSplit sp = fier::prompt_split(a.units, a.n_rep, a.max_new, a.kv_cap);
-  a.side_parts = sp.side_parts, a.shared_parts = sp.shared_parts;
   const Workspace w = carve(cfg, 1, workspace);
   a.counters = w.sb.hist;
   a.side_partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.zero_bytes);
-  a.shared_partials = a.side_partials + sp.side_floats;
-  return fier::launch_prompt_attn(cfg->kv_dtype, a, (hipStream_t)stream);
+  return fier::launch_prompt_attn(cfg->kv_dtype, a, prompt_split(cfg, n_tokens, max_new, true), (hipStream_t)stream);
 }
 
 size_t fier_chunk_workspace_bytes(const fier_config* cfg, int32_t n_tokens, int32_t max_new) {
   if (check_cfg(cfg) != FIER_OK || n_tokens < 0 || n_tokens > kMaxNewTokens || max_new < 0) return 0;
-  const fier::PromptSplit sp = fier::prompt_split(units_of(cfg), n_rep_of(cfg), std::min(max_new, n_tokens), cfg->max_ctx);
+  const fier::PromptSplit sp = prompt_split(cfg, n_tokens, max_new, true);
   return carve(cfg, 1, nullptr).zero_bytes + align_up((sp.side_floats + sp.shared_floats) * sizeof(float));
 }
 

@@ -183,11 +183,11 @@ __device__ __forceinline__ unsigned long long load_coherent(const unsigned long 
 
 // Arrival at a unit's counter: adds `inc` and returns, in every thread, the value the counter held before.
 // Everything the workgroups that arrived earlier published with store_coherent / atomics before arriving can then be
-// read with load_coherent.  Nobody waits for anybody.  flag: one word of LDS.
-__device__ __forceinline__ uint32_t arrive_add(uint32_t* counter, uint32_t inc, uint32_t* flag) {
+// read with load_coherent.  Nobody waits for anybody.  flag: one word of LDS.  first: true in one thread.
+__device__ __forceinline__ uint32_t arrive_add(uint32_t* counter, uint32_t inc, uint32_t* flag, bool first) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores and atomics have been acknowledged
   __syncthreads();                                  // ... and so have those of the other waves
-  if (threadIdx.x == 0) *flag = __hip_atomic_fetch_add(counter, inc, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (first) *flag = __hip_atomic_fetch_add(counter, inc, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   const uint32_t before = *flag;
   // reader side: nothing the last arriver loads afterwards may be moved above the counter's return by the compiler
@@ -195,6 +195,9 @@ __device__ __forceinline__ uint32_t arrive_add(uint32_t* counter, uint32_t inc, 
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
   asm volatile("" ::: "memory");
   return before;
+}
+__device__ __forceinline__ uint32_t arrive_add(uint32_t* counter, uint32_t inc, uint32_t* flag) {
+  return arrive_add(counter, inc, flag, threadIdx.x == 0);
 }
 // "Last arriver": true in every thread of exactly one workgroup per counter, the one whose increment brings it to
 // `expected`.

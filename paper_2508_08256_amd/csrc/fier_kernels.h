@@ -229,11 +229,11 @@ struct PromptArgs {  // attention of the new tokens (passed to the kernel by val
   KvLayout lay;
   float scale;   // softmax scale * log2(e), positive
   uint32_t flip, keep;  // sign bits to flip (negative scales) and bits to keep (none for a scale of 0) of the queries
-  int units, n_kv_heads, n_q_heads, n_rep;
+  int batch, n_kv_heads, n_q_heads, n_rep;
   int n_tokens, max_new, kv_cap;  // kv_cap: rows of a cache; no limit without one
-  int row_tiles, side_parts, shared_parts;  // see PromptSplit
   float *side_partials, *shared_partials;
   uint32_t* counters;  // kSelBins words per unit, zero between calls
+  int side_grid, side_parts, shared_parts, side_slots, shared_slots;  // from PromptSplit
   bool from_cache;
   // Whatever the offsets hold, the span lies inside the n_tokens rows.
   __device__ __forceinline__ PromptSpan span(int b) const {
@@ -247,15 +247,15 @@ struct PromptArgs {  // attention of the new tokens (passed to the kernel by val
     return w;
   }
 };
-// FIER_OK, FIER_EHIP, or FIER_ESHAPE for a grid that does not fit 32 bits.
-int launch_prompt_attn(int dtype, const PromptArgs& a, hipStream_t st);
 struct PromptSplit {  // how the launch is cut
-  int row_tiles;     // workgroups for a unit's query rows, without the one for up to 32 rows that are left
-  int side_parts;    // parts that those 32 rows' K / V rows are split into, at most
-  int shared_parts;  // and those of the others
-  size_t side_floats, shared_floats;  // partial results
+  int64_t side_grid, shared_grid;     // workgroups
+  int side_parts, shared_parts;       // parts of K / V rows wanted per kv head; 0: nothing is split
+  int side_slots, shared_slots;       // partial results per kv head
+  size_t side_floats, shared_floats;  // of all of them
 };
-PromptSplit prompt_split(int units, int n_rep, int max_new, int kv_cap);
+PromptSplit prompt_split(int batch, int n_kv_heads, int n_rep, int n_tokens, int max_new, bool split);
+// FIER_OK, FIER_EHIP, or FIER_ESHAPE for a grid that does not fit 32 bits.
+int launch_prompt_attn(int dtype, PromptArgs a, const PromptSplit& sp, hipStream_t st);
 
 // ---- page-level importance (comparison workload) -------------------------------------------------------------------
 hipError_t launch_page_minmax(int dtype, KvLayout lay, const void* K, const int32_t* seq_lens, uint32_t* page_meta, int units,

@@ -119,24 +119,36 @@ struct UnitRows {
   __device__ __forceinline__ size_t row(int block, int t) const { return (size_t)block * block_stride + (size_t)(t & mask); }
 };
 
-// The N instructions of a wavefront that bring its share of a tile: rows 4 (N0 + STEP j) .. + 3.
+// A wavefront's share of a tile: N instructions, rows 4 (n0 + STEP j) .. + 3 of instruction j.  The permutation of a row's chunks
+// repeats after 16 rows (V: 8): as many offsets differ in more than the rows' distance, which goes into the scalar address.
 template <bool V, int N, int STEP>
 struct RowLoads {
-  uint32_t chunk[N];  // offset of the lane's 16 bytes in its row; repeats where the permutation does
-  int row[N];
-  __device__ __forceinline__ RowLoads(int n0, int lane) {
+  static constexpr int kCycle = (V ? 8 : 16) / 4 / STEP > 1 ? (V ? 8 : 16) / 4 / STEP : 1;
+  uint32_t off[kCycle];
+  __device__ __forceinline__ static uint32_t chunk(int row, int lane) {
+    const int c = lane & 15;
+    return 16u * (uint32_t)(V ? c ^ (((row & 3) << 2) | ((row >> 1) & 2)) : c ^ (row & 15));
+  }
+  __device__ __forceinline__ RowLoads(int n0, int lane, int64_t stride) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      row[j] = 4 * (n0 + STEP * j) + (lane >> 4);
-      const int c = lane & 15;
-      chunk[j] = 16u * (uint32_t)(V ? c ^ (((row[j] & 3) << 2) | ((row[j] >> 1) & 2)) : c ^ (row[j] & 15));
+    for (int j = 0; j < kCycle; ++j) {
+      const int row = 4 * (n0 + STEP * j) + (lane >> 4);
+      off[j] = (uint32_t)row * (uint32_t)stride + chunk(row, lane);
     }
   }
   // rows: how many the tile has; the others take the last one's (they get no weight)
-  __device__ __forceinline__ void load(const char* src, int64_t stride, int rows, const lds_char* dst, int n0) const {
+  __device__ __forceinline__ void load(const char* src, int64_t stride, int rows, const lds_char* dst, int n0, int lane) const {
+    if (rows >= 4 * N * STEP) {
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      load_rows_to_lds(src, (uint32_t)min(row[j], rows - 1) * (uint32_t)stride + chunk[j], dst + 4 * (n0 + STEP * j) * kRowBytes);
+      for (int j = 0; j < N; ++j)
+        load_rows_to_lds(src + (int64_t)(4 * STEP * (j / kCycle * kCycle)) * stride, off[j % kCycle], dst + 4 * (n0 + STEP * j) * kRowBytes);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int row = 4 * (n0 + STEP * j) + (lane >> 4);
+        load_rows_to_lds(src, (uint32_t)min(row, rows - 1) * (uint32_t)stride + chunk(row, lane), dst + 4 * (n0 + STEP * j) * kRowBytes);
+      }
+    }
   }
 };
 
@@ -236,6 +248,13 @@ __device__ __forceinline__ void store_channels(char* out_row, int ct, int h, con
         make_uint2(pack2<DT>(o[4 * i] * inv, o[4 * i + 1] * inv), pack2<DT>(o[4 * i + 2] * inv, o[4 * i + 3] * inv));
 }
 
+// The lane's number anew: what is only needed after a loop need not live in registers through it.
+__device__ __forceinline__ int lane_again() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
 // ---- one query row per lane and half ------------------------------------------------------------------------------------
 struct QueryRow {
   const char* q;
@@ -310,154 +329,220 @@ __device__ __forceinline__ void join_partials(const float* slots, size_t pitch, 
   }
 }
 
-// The parts that n_tiles steps are split into, at most `most`, none shorter than `least` steps.
-__device__ __forceinline__ int parts_of(int n_tiles, int most, int least) { return max(1, min(most, n_tiles / least)); }
-
 constexpr int kSideTile = 32;    // rows of K and V per wavefront and step where the wavefronts go side by side
-constexpr int kSideLeast = 2;    // steps of 128 rows of such a part, at least
+constexpr int kSideWaves = 3;    // of four: three such workgroups fit a CU's LDS
+constexpr int kSideStep = kSideWaves * kSideTile;
+#ifndef MAXP
+#define MAXP 48
+#endif
+constexpr int kMostParts = MAXP;  // of a tile
+constexpr int kSideLeast = 2;    // steps of a part there, at least
 constexpr int kSharedLeast = 8;  // steps of 64 rows of a part where the wavefronts share the tiles, at least
 
-// Up to 32 query rows: all four wavefronts hold them and go side by side through the K / V rows, each through 32 of every 128,
-// in 16 KiB of LDS of its own, so that nobody waits for anybody.  The next K rows are loaded once this step's logits are
-// there, the next V rows after its product.  Bound by memory.
+// ---- which workgroup does what -----------------------------------------------------------------------------------------------
+// A sequence's query rows per kv head are cut into tiles of 128; the last one, where it has at most 32, goes through its K / V
+// rows side by side, the others share them.  Where there are partial results to hand on (a cache's workspace), the K / V rows of
+// a tile are split into parts of `step` steps, one length for all sequences of the call, so that unequal ones keep the GPU busy to
+// the end: `step` is the call's steps over the number of parts wanted.  Lengths lie on the GPU, so every workgroup works
+// this out for itself, one sequence a lane.
+struct SequenceWork {
+  PromptSpan sp;
+  int n_rows, tiles, aside;  // tiles of shared rows; rows of the side-by-side tile or 0
+  int n_kv;                  // rows of K and V that the last query row attends over
+  // tokens: of the sequences in front of the lanes' ones, 64 more of them afterwards.  Offsets that do not ascend can make
+  // sequences share tokens: those with which there would be more than n_tokens of them in all count as empty, so that the grid
+  // always holds every item and no split tile is left without one of its parts.
+  __device__ __forceinline__ SequenceWork(const PromptArgs& a, int b, int lane, int64_t& tokens) {
+    sp = PromptSpan{0, 0, 0};
+    if (b < a.batch) sp = a.span(b);
+    const uint32_t upto = wave_incl_scan_u32((uint32_t)sp.n, lane);
+    if (tokens + upto > (int64_t)a.n_tokens) sp.n = 0;
+    tokens += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    n_rows = sp.n * a.n_rep;
+    const int rest = n_rows % kRowTile;
+    aside = rest <= kSideRows ? rest : 0;
+    tiles = n_rows / kRowTile + (rest > kSideRows ? 1 : 0);
+    n_kv = min(sp.first + sp.n, a.kv_cap);
+  }
+  template <bool SIDE>
+  __device__ __forceinline__ int steps() const {  // of the last tile
+    return SIDE ? (n_kv + kSideStep - 1) / kSideStep : (n_kv + kTile - 1) / kTile;
+  }
+  template <bool SIDE>
+  __device__ __forceinline__ int parts(int step) const {  // that its tiles have at most; more tiles than counters: not split
+    const int n = steps<SIDE>();
+    return n <= step || (!SIDE && tiles >= kSelBins - 1) ? 1 : min((n + step - 1) / step, kMostParts);
+  }
+  template <bool SIDE>
+  __device__ __forceinline__ int items(int step) const {
+    return SIDE ? (aside ? parts<true>(step) : 0) : tiles * parts<false>(step);
+  }
+};
+struct Item {
+  PromptSpan sp;
+  int b, at;    // sequence; which of its items
+  int parts;    // of its tiles
+  int step;     // steps of a part
+  int slot;     // partial results: the place of the sequence's first item
+};
+// Sum of the lanes' values, the same in every lane and workgroup.
+__device__ __forceinline__ float wave_sum_ordered(float x) {
+  x += row_ror<8>(x), x += row_ror<4>(x), x += row_ror<2>(x), x += row_ror<1>(x);
+  const int v = __float_as_int(x);
+  return (__int_as_float(__builtin_amdgcn_readlane(v, 0)) + __int_as_float(__builtin_amdgcn_readlane(v, 16))) +
+         (__int_as_float(__builtin_amdgcn_readlane(v, 32)) + __int_as_float(__builtin_amdgcn_readlane(v, 48)));
+}
+// Item number j of the launch's (per kv head); false: there are fewer.
+template <bool SIDE>
+__device__ __forceinline__ bool find_item(const PromptArgs& a, int j, int lane, Item& it) {
+  const int wanted = SIDE ? a.side_parts : a.shared_parts;  // 0: nothing is split
+  it.step = 1 << 30;
+  if (wanted) {
+    float all = 0.f;
+    int64_t tokens = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+      const SequenceWork w(a, b0 + lane, lane, tokens);
+      all += wave_sum_ordered((float)(SIDE ? (w.aside ? 1 : 0) : w.tiles) * (float)w.steps<SIDE>());
+    }
+    it.step = max(SIDE ? kSideLeast : kSharedLeast, (int)ceilf(all / (float)wanted));
+    it.step = __builtin_amdgcn_readfirstlane(it.step);
+  }
+  int before = 0, slots = 0;
+  int64_t tokens = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const SequenceWork w(a, b0 + lane, lane, tokens);
+    const int parts = w.parts<SIDE>(it.step), n = w.items<SIDE>(it.step), split = parts > 1 ? n : 0;
+    const int upto = before + (int)wave_incl_scan_u32((uint32_t)n, lane);
+    const int slots_upto = slots + (int)wave_incl_scan_u32((uint32_t)split, lane);
+    const unsigned long long past = __ballot(upto > j);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      it.b = b0 + l;
+      it.sp = PromptSpan{__builtin_amdgcn_readlane(w.sp.lo, l), __builtin_amdgcn_readlane(w.sp.n, l), __builtin_amdgcn_readlane(w.sp.first, l)};
+      it.at = j - __builtin_amdgcn_readlane(upto - n, l);
+      it.parts = __builtin_amdgcn_readlane(parts, l);
+      it.slot = __builtin_amdgcn_readlane(slots_upto - split, l);
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+    slots = __builtin_amdgcn_readlane(slots_upto, 63);
+  }
+  return false;
+}
+
+
+// The wavefronts' results of a side-by-side tile: each puts its own into its LDS, then takes one channel tile of all.
 template <int DT>
-__device__ __forceinline__ void attend_side_by_side(const PromptArgs& a, const PromptSpan& sp, int unit, int head, int row0,
-                                                    int n_rows, int part, lds_char* lds, uint32_t* flag) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 31, h = lane >> 5;
-  const int n_kv = min(sp.first + (n_rows - 1) / a.n_rep + 1, a.kv_cap);
-  const int all = (n_kv + 127) / 128, n_parts = parts_of(all, a.side_parts, kSideLeast);
-  if (part >= n_parts) return;
-  const int begin = (int)((int64_t)all * part / n_parts), end = (int)((int64_t)all * (part + 1) / n_parts);
-  const QueryRow row(a, sp, head, row0 + n, n_rows);
-  const int least = __builtin_amdgcn_readfirstlane(row.lim);  // the first row's
-  const UnitRows rows(a, unit, head, sp.lo);
-  lds_char* const kt = lds + wave * 2 * kSideTile * kRowBytes;
-  lds_char* const vt = kt + kSideTile * kRowBytes;
-  const RowLoads<false, 8, 1> kl(0, lane);
-  const RowLoads<true, 8, 1> vl(0, lane);
-  int t0 = begin * 128 + wave * kSideTile;
-  const int stop = min(end * 128, n_kv);
-  int block = 0;
-  if (t0 < stop) {
-    const size_t r = rows.row(rows.block_of(t0), t0);
-    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - t0, kt, 0);
-    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - t0, vt, 0);
-    block = rows.block_of(t0 + 128 < stop ? t0 + 128 : t0);
-  }
-  uint4 q[8];
-#pragma unroll
-  for (int s = 0; s < 8; ++s) q[s] = a.load_q(row.q + s * 32 + h * 16);
-  Rows32<DT> st;
-  st.init();
-  for (; t0 < stop; t0 += 128) {
-    const int next = t0 + 128 < stop ? t0 + 128 : t0;  // the last step loads its own rows once more
-    const size_t r = rows.row(block, next);
-    floatx16_t s[1];
-    wait_loads<8>();
-    Rows32<DT>::scores(kt, q, n, h, s);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, kt, 0);
-    block = rows.block_of(next + 128 < stop ? next + 128 : next);  // for the step after the next: the list is far away
-    st.weights(s, a.scale, t0 + kSideTile > least, row.lim - t0, h);
-    wait_loads<8>();
-    st.add_values(vt, s, lane, h);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - next, vt, 0);
-  }
-  wait_loads<0>();
-  // the four wavefronts' results: each puts its own into its LDS, then takes one channel tile of all
+__device__ __forceinline__ void join_side_by_side(const PromptArgs& a, const Item& it, int head, const Rows32<DT>& st, int wave,
+                                                  lds_char* lds, uint32_t* flag) {
+  const int lane = lane_again(), h = lane >> 5;
+  const int unit = it.b * a.n_kv_heads + head, n_rows = it.sp.n * a.n_rep, part = it.at, n_parts = it.parts;
+  const QueryRow row(a, it.sp, head, n_rows / kRowTile * kRowTile + (lane & 31), n_rows);
   const float l = halves_sum(st.l);
-  __attribute__((address_space(3))) float* const mine = (__attribute__((address_space(3))) float*)kt;
-#pragma unroll
-  for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) mine[(ct * 16 + i) * 64 + lane] = st.o[ct][i];
-  __attribute__((address_space(3))) float2* const ml = (__attribute__((address_space(3))) float2*)(lds + 8 * kSideTile * kRowBytes);
+  typedef __attribute__((address_space(3))) float lds_float;
   typedef float f2_t __attribute__((ext_vector_type(2)));
-  *(__attribute__((address_space(3))) f2_t*)&ml[wave * 64 + lane] = f2_t{st.m, l};
+  typedef __attribute__((address_space(3))) f2_t lds_f2;
+  lds_f2* const ml = (lds_f2*)(lds + 2 * kSideStep * kRowBytes);
+  if (wave < kSideWaves) {
+    lds_float* const mine = (lds_float*)(lds + wave * 2 * kSideTile * kRowBytes);
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mine[(ct * 16 + i) * 64 + lane] = st.o[ct][i];
+    ml[wave * 64 + lane] = f2_t{st.m, l};
+  }
   meet();
   float m = -FLT_MAX, sum = 0.f;
-  f2_t of[4];
+  f2_t of[kSideWaves];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    of[w] = *(__attribute__((address_space(3))) f2_t*)&ml[w * 64 + lane];
+  for (int w = 0; w < kSideWaves; ++w) {
+    of[w] = ml[w * 64 + lane];
     m = fmaxf(m, of[w].x);
   }
   floatx16_t o[1] = {floatx16_t{0.f}};
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < kSideWaves; ++w) {
     const float f = __builtin_amdgcn_exp2f(of[w].x - m);
     sum += f * of[w].y;
-    const __attribute__((address_space(3))) float* const p = (const __attribute__((address_space(3))) float*)(lds + w * 2 * kSideTile * kRowBytes);
+    const lds_float* const p = (const lds_float*)(lds + w * 2 * kSideTile * kRowBytes);
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[0][i] += f * p[(wave * 16 + i) * 64 + lane];
   }
   if (n_parts > 1) {
-    float* const slots = a.side_partials + (size_t)unit * a.side_parts * kPartFloats;
+    float* const slots = a.side_partials + ((size_t)head * a.side_slots + it.slot) * kPartFloats;
     if (row.there) {
       store_partial(slots + (size_t)part * kPartFloats, wave, o[0], lane);
       if (wave == 0) store_partial_sums(slots + (size_t)part * kPartFloats, m, sum, lane);
     }
     uint32_t* const counter = a.counters + (size_t)unit * kSelBins;
-    if (!last_arriver(counter, (uint32_t)n_parts, flag)) return;
+    if (arrive_add(counter, 1u, flag, wave == 0 && lane == 0) != (uint32_t)n_parts - 1) return;  // not the last one
     if (row.there) join_partials<1, 8>(slots, kPartFloats, n_parts, wave, lane, o, sum);
-    if (threadIdx.x == 0) store_coherent(counter, 0u);
+    if (wave == 0 && lane == 0) store_coherent(counter, 0u);
   }
   if (row.there) store_channels<DT>(row.out, wave, h, o[0], sum > 0.f ? 1.f / sum : 0.f);
 }
 
-// 128 query rows, 32 a wavefront; the K / V rows go through LDS 64 at a time, two tiles of each, shared by the wavefronts.
+// Up to 32 query rows: all four wavefronts hold them and go side by side through the K / V rows, each through 32 of every 128,
+// in 16 KiB of LDS of its own, so that nobody waits for anybody.  The next K rows are loaded once this step's logits are
+// there, the next V rows after its product.  Bound by memory.
 template <int DT>
-__device__ __forceinline__ void attend_shared(const PromptArgs& a, const PromptSpan& sp, int unit, int head, int tile,
-                                              int n_rows, int part, lds_char* lds, uint32_t* flag) {
+__device__ __forceinline__ void attend_side_by_side(const PromptArgs& a, const Item& it, int head, lds_char* lds, uint32_t* flag) {
+  const PromptSpan sp = it.sp;
+  const int unit = it.b * a.n_kv_heads + head, n_rows = sp.n * a.n_rep, row0 = n_rows / kRowTile * kRowTile;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
-  const int row0 = tile * kRowTile;
-  const int n_kv = min(sp.first + (min(row0 + kRowTile, n_rows) - 1) / a.n_rep + 1, a.kv_cap);
-  const int all = (n_kv + kTile - 1) / kTile, n_parts = parts_of(all, a.shared_parts, kSharedLeast);
-  if (part >= n_parts) return;
-  const int begin = (int)((int64_t)all * part / n_parts), end = (int)((int64_t)all * (part + 1) / n_parts);
-  const QueryRow row(a, sp, head, row0 + wave * 32 + n, n_rows);
-  const int least = __builtin_amdgcn_readfirstlane(row.lim), most = __builtin_amdgcn_readlane(row.lim, 31);
+  const int n_kv = min(sp.first + (n_rows - 1) / a.n_rep + 1, a.kv_cap);
+  const int all = (n_kv + kSideStep - 1) / kSideStep, n_parts = it.parts;
+  const int begin = (int)((int64_t)all * it.at / n_parts), end = (int)((int64_t)all * (it.at + 1) / n_parts);
+  const QueryRow row(a, sp, head, row0 + n, n_rows);
+  const int least = __builtin_amdgcn_readfirstlane(row.lim);  // the first row's
   const UnitRows rows(a, unit, head, sp.lo);
-  constexpr int kBytes = kTile * kRowBytes;
-  const RowLoads<false, 4, 4> kl(wave, lane);
-  const RowLoads<true, 4, 4> vl(wave, lane);
-  const size_t r0 = rows.row(rows.block_of(begin * kTile), begin * kTile);
-  kl.load(rows.k + r0 * rows.k_stride, rows.k_stride, n_kv - begin * kTile, lds, wave);
-  vl.load(rows.v + r0 * rows.v_stride, rows.v_stride, n_kv - begin * kTile, lds + 2 * kBytes, wave);
-  int block = rows.block_of(min(begin + 1, end - 1) * kTile);
+  lds_char* const kt = lds + wave * 2 * kSideTile * kRowBytes;
+  lds_char* const vt = kt + kSideTile * kRowBytes;
+  const RowLoads<false, 8, 1> kl(0, lane, rows.k_stride);
+  const RowLoads<true, 8, 1> vl(0, lane, rows.v_stride);
+  int t0 = begin * kSideStep + wave * kSideTile;
+  const int stop = wave < kSideWaves ? min(end * kSideStep, n_kv) : 0;
+  int block = 0;
+  if (t0 < stop) {
+    const size_t r = rows.row(rows.block_of(t0), t0);
+    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - t0, kt, 0, lane);
+    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - t0, vt, 0, lane);
+    block = rows.block_of(t0 + kSideStep < stop ? t0 + kSideStep : t0);
+  }
   uint4 q[8];
 #pragma unroll
   for (int s = 0; s < 8; ++s) q[s] = a.load_q(row.q + s * 32 + h * 16);
   Rows32<DT> st;
   st.init();
-  for (int i = begin; i < end; ++i) {
-    const int t0 = i * kTile, next = i + 1 < end ? t0 + kTile : t0, cur = (i - begin) & 1;
-    lds_char* const kt = lds + cur * kBytes;
-    lds_char* const vt = lds + (2 + cur) * kBytes;
+  for (; t0 < stop; t0 += kSideStep) {
+    const int next = t0 + kSideStep < stop ? t0 + kSideStep : t0;  // the last step loads its own rows once more
     const size_t r = rows.row(block, next);
-    const bool needed = t0 < most;  // none of the wavefront's rows goes that far
-    floatx16_t s[2];
-    wait_loads<4>();
-    meet();
-    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, lds + (cur ^ 1) * kBytes, wave);
-    block = rows.block_of(min(i + 2, end - 1) * kTile);
-    if (needed) {
-      Rows32<DT>::scores(kt, q, n, h, s);
-      st.weights(s, a.scale, t0 + kTile > least, row.lim - t0, h);
-    }
-    wait_loads<4>();
-    meet();
-    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - next, lds + (2 + (cur ^ 1)) * kBytes, wave);
-    if (needed) st.add_values(vt, s, lane, h);
+    floatx16_t s[1];
+    wait_loads<8>();
+    Rows32<DT>::scores(kt, q, n, h, s);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, kt, 0, lane);
+    block = rows.block_of(next + kSideStep < stop ? next + kSideStep : next);  // for the step after the next: the list is far away
+    st.weights(s, a.scale, t0 + kSideTile > least, row.lim - t0, h);
+    wait_loads<8>();
+    st.add_values(vt, s, lane, h);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - next, vt, 0, lane);
   }
   wait_loads<0>();
+  join_side_by_side<DT>(a, it, head, st, wave, lds, flag);
+}
+// The results of a tile of shared rows, through partial results where its K / V rows were split.
+template <int DT>
+__device__ __forceinline__ void finish_shared(const PromptArgs& a, const Item& it, int head, int tile, int turned, int part, int n_parts,
+                                              Rows32<DT>& st, int wave, uint32_t* flag) {
+  const int lane = lane_again(), h = lane >> 5;
+  const int unit = it.b * a.n_kv_heads + head;
+  const QueryRow row(a, it.sp, head, tile * kRowTile + wave * 32 + (lane & 31), it.sp.n * a.n_rep);
   float l = halves_sum(st.l);
   if (n_parts > 1) {
-    const size_t item = (size_t)unit * a.row_tiles + tile;
-    float* const slots = a.shared_partials + (item * a.shared_parts * 4 + wave) * kPartFloats;
+    float* const slots = a.shared_partials + (((size_t)head * a.shared_slots + it.slot + turned * it.parts) * 4 + wave) * kPartFloats;
     if (row.there) {
       float* const slot = slots + (size_t)part * 4 * kPartFloats;
 #pragma unroll
@@ -465,9 +550,9 @@ __device__ __forceinline__ void attend_shared(const PromptArgs& a, const PromptS
       store_partial_sums(slot, st.m, l, lane);
     }
     uint32_t* const counter = a.counters + (size_t)unit * kSelBins + 1 + tile;
-    if (!last_arriver(counter, (uint32_t)n_parts, flag)) return;
+    if (arrive_add(counter, 1u, flag, wave == 0 && lane == 0) != (uint32_t)n_parts - 1) return;  // not the last one
     if (row.there) join_partials<4, 2>(slots, 4 * kPartFloats, n_parts, 0, lane, st.o, l);
-    if (threadIdx.x == 0) store_coherent(counter, 0u);
+    if (wave == 0 && lane == 0) store_coherent(counter, 0u);
   }
   if (!row.there) return;
   const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -475,52 +560,116 @@ __device__ __forceinline__ void attend_shared(const PromptArgs& a, const PromptS
   for (int ct = 0; ct < 4; ++ct) store_channels<DT>(row.out, ct, h, st.o[ct], inv);
 }
 
-// The query rows of a unit are cut into tiles of 128; the last one, where it has at most 32, goes through its K / V rows side by
-// side.  The grid lists a place for that one of every unit first, side_parts times, then the whole tiles, the last ones (which
-// attend over the most rows) first; units fastest, so that with a multiple of 8 units a unit's K and V stay in one XCD's L2.
-// What has no work leaves at once.  A tile whose K / V rows are split hands its partial results to the last of its workgroups.
+// 128 query rows, 32 a wavefront; the K / V rows go through LDS 64 at a time, two tiles of each, shared by the wavefronts.
 template <int DT>
-__global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptArgs a) {
-  __shared__ __attribute__((aligned(16))) char lds[4 * kTile * kRowBytes + 4 * 64 * 8];
-  __shared__ uint32_t flag;
-  const unsigned id = blockIdx.x, side = (unsigned)a.units * (unsigned)a.side_parts;
-  const unsigned place = (id < side ? id : id - side) / (unsigned)a.units;
-  const int unit = (int)((id < side ? id : id - side) - place * (unsigned)a.units);
-  const int b = unit / a.n_kv_heads, head = unit - b * a.n_kv_heads;
-  PromptSpan sp = a.span(b);
-  sp = {__builtin_amdgcn_readfirstlane(sp.lo), __builtin_amdgcn_readfirstlane(sp.n), __builtin_amdgcn_readfirstlane(sp.first)};
-  const int n_rows = sp.n * a.n_rep, whole = n_rows / kRowTile, rest = n_rows - whole * kRowTile;
-  const bool aside = rest > 0 && rest <= kSideRows;
-  if (id < side) {
-    if (aside) attend_side_by_side<DT>(a, sp, unit, head, whole * kRowTile, n_rows, (int)place, (lds_char*)lds, &flag);
-    return;
+__device__ __forceinline__ void attend_shared(const PromptArgs& a, const Item& it, int head, lds_char* lds, uint32_t* flag) {
+  const PromptSpan sp = it.sp;
+  const int unit = it.b * a.n_kv_heads + head, n_rows = sp.n * a.n_rep;
+  const int tiles = n_rows / kRowTile + (n_rows % kRowTile > kSideRows ? 1 : 0);
+  // the tiles that attend over the most rows first
+  const int turned = it.at / it.parts, tile = tiles - 1 - turned, part = it.at - turned * it.parts;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  const int row0 = tile * kRowTile;
+  const int n_kv = min(sp.first + (min(row0 + kRowTile, n_rows) - 1) / a.n_rep + 1, a.kv_cap);
+  const int all = (n_kv + kTile - 1) / kTile, n_parts = min(it.parts, (all + it.step - 1) / it.step);
+  if (part >= n_parts) return;  // the first tiles of a prompt attend over fewer rows than the last one
+  const int begin = (int)((int64_t)all * part / n_parts), end = (int)((int64_t)all * (part + 1) / n_parts);
+  const QueryRow row(a, sp, head, row0 + wave * 32 + n, n_rows);
+  const int least = __builtin_amdgcn_readfirstlane(row.lim), most = __builtin_amdgcn_readlane(row.lim, 31);
+  const UnitRows rows(a, unit, head, sp.lo);
+  constexpr int kBytes = kTile * kRowBytes;
+  const RowLoads<false, 4, 4> kl(wave, lane, rows.k_stride);
+  const RowLoads<true, 4, 4> vl(wave, lane, rows.v_stride);
+  const size_t r0 = rows.row(rows.block_of(begin * kTile), begin * kTile);
+  kl.load(rows.k + r0 * rows.k_stride, rows.k_stride, n_kv - begin * kTile, lds, wave, lane);
+  size_t r = r0;
+  int block = rows.block_of(min(begin + 1, end - 1) * kTile);
+  uint4 q[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) q[s] = a.load_q(row.q + s * 32 + h * 16);
+  Rows32<DT> st;
+  st.init();
+  lds_char* const vt = lds + 2 * kBytes;
+  for (int i = begin; i < end; ++i) {
+    const int t0 = i * kTile, next = i + 1 < end ? t0 + kTile : t0, cur = (i - begin) & 1;
+    const lds_char* const kt = lds + cur * kBytes;
+    wait_loads<0>();
+    meet();
+    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - t0, vt, wave, lane);
+    r = rows.row(block, next);
+    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, lds + (cur ^ 1) * kBytes, wave, lane);
+    block = rows.block_of(min(i + 2, end - 1) * kTile);
+    floatx16_t s[1];
+    if (t0 < most) {  // some of the wavefront's rows go that far
+      Rows32<DT>::scores(kt, q, n, h, s);
+      st.weights(s, a.scale, t0 + 32 > least, row.lim - t0, h);
+    }
+    wait_loads<4>();
+    meet();
+    if (t0 < most) st.add_values(vt, s, lane, h);
+    if (t0 + 32 < most) {
+      Rows32<DT>::scores(kt + 32 * kRowBytes, q, n, h, s);
+      st.weights(s, a.scale, t0 + kTile > least, row.lim - t0 - 32, h);
+      st.add_values(vt + 32 * kRowBytes, s, lane, h);
+    }
   }
-  const int tile = a.row_tiles - 1 - (int)(place / (unsigned)a.shared_parts);
-  if (tile < whole || (tile == whole && rest > kSideRows))
-    attend_shared<DT>(a, sp, unit, head, tile, n_rows, (int)(place % (unsigned)a.shared_parts), (lds_char*)lds, &flag);
+  wait_loads<0>();
+  finish_shared<DT>(a, it, head, tile, turned, part, n_parts, st, wave, flag);
 }
 
-// How many parts the K / V rows are split into, and the workspace for them.
-PromptSplit prompt_split(int units, int n_rep, int max_new, int kv_cap) {
-  PromptSplit sp;
-  const int64_t rows = (int64_t)max_new * n_rep;
-  sp.row_tiles = (int)((rows + kRowTile - 1) / kRowTile);
-  if (rows <= kSideRows) sp.row_tiles = 0;  // every unit's rows go side by side
-  const int64_t tiles = (int64_t)units * sp.row_tiles;
-  sp.side_parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(2048 / units, 64), kv_cap / (128 * kSideLeast)));
-  sp.shared_parts = tiles == 0 || sp.row_tiles >= kSelBins - 1
-                        ? 1
-                        : (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, kv_cap / (kTile * kSharedLeast)));
-  sp.side_floats = sp.side_parts > 1 ? (size_t)units * sp.side_parts * kPartFloats : 0;
-  sp.shared_floats = sp.shared_parts > 1 ? (size_t)tiles * sp.shared_parts * 4 * kPartFloats : 0;
+// The grid lists the side-by-side items first, then the shared ones, the kv heads of an item next to each other: with a multiple
+// of 8 of them a head's K and V stay in one XCD's L2.  What has no work leaves at once.  A tile whose K / V rows are split hands
+// its partial results to the last of its workgroups.
+template <int DT>
+__global__ __launch_bounds__(256, 3) void prompt_attn_kernel(PromptArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[3 * kTile * kRowBytes + kSideWaves * 64 * 8];
+  __shared__ uint32_t flag;
+  const int lane = threadIdx.x & 63;
+  const bool side = blockIdx.x < (unsigned)a.side_grid;
+  const unsigned id = side ? blockIdx.x : blockIdx.x - (unsigned)a.side_grid;
+  const int j = (int)(id / (unsigned)a.n_kv_heads), head = (int)(id - (unsigned)j * (unsigned)a.n_kv_heads);
+  Item it;
+  if (side) {
+    if (find_item<true>(a, j, lane, it)) attend_side_by_side<DT>(a, it, head, (lds_char*)lds, &flag);
+  } else {
+    if (find_item<false>(a, j, lane, it)) attend_shared<DT>(a, it, head, (lds_char*)lds, &flag);
+  }
+}
+
+#ifndef SIDE_T
+#define SIDE_T 1536
+#endif
+#ifndef SHARED_T
+#define SHARED_T 768
+#endif
+// How the launch is cut.
+PromptSplit prompt_split(int batch, int n_kv_heads, int n_rep, int n_tokens, int max_new, bool split) {
+  PromptSplit sp = {};
+  const int64_t rows = (int64_t)max_new * n_rep, all_rows = (int64_t)n_tokens * n_rep;
+  const bool shared = rows > kSideRows;  // some sequence may have more rows than go side by side
+  const int64_t seqs = std::min(batch, n_tokens);
+  sp.side_parts = split ? std::max(1, SIDE_T / n_kv_heads) : 0;
+  sp.shared_parts = split && shared ? std::max(1, SHARED_T / n_kv_heads) : 0;
+  sp.side_grid = (seqs + sp.side_parts) * n_kv_heads;
+  sp.shared_grid = shared ? (all_rows / kRowTile + seqs + sp.shared_parts) * n_kv_heads : 0;
+  // Items of tiles in more than one part: at most twice the parts wanted, since ceil(x) < 2 x for x > 1.
+  sp.side_slots = 2 * sp.side_parts;
+  sp.shared_slots = 2 * sp.shared_parts;
+  sp.side_floats = (size_t)sp.side_slots * n_kv_heads * kPartFloats;
+  sp.shared_floats = (size_t)sp.shared_slots * n_kv_heads * 4 * kPartFloats;
   return sp;
 }
 
 // FIER_ESHAPE where the grid would not fit 32 bits, else FIER_OK or FIER_EHIP.
-int launch_prompt_attn(int dtype, const PromptArgs& a, hipStream_t st) {
-  const int64_t grid = (int64_t)a.units * a.side_parts + (int64_t)a.units * a.row_tiles * a.shared_parts;
+int launch_prompt_attn(int dtype, PromptArgs a, const PromptSplit& sp, hipStream_t st) {
+  const int64_t grid = sp.side_grid + sp.shared_grid;
   if (a.max_new == 0) return FIER_OK;
   if (grid > INT32_MAX) return FIER_ESHAPE;
+  a.side_grid = (int)sp.side_grid;
+  a.side_parts = sp.side_parts, a.shared_parts = sp.shared_parts;
+  a.side_slots = sp.side_slots, a.shared_slots = sp.shared_slots;
+  a.shared_partials = a.side_partials + sp.side_floats;
   if (dtype == DT_F16)
     prompt_attn_kernel<DT_F16><<<(unsigned)grid, 256, 0, st>>>(a);
   else
