@@ -618,6 +618,7 @@ static fier::PromptArgs prompt_args(const fier_config* cfg, const void* q, int64
   a.n_kv_heads = cfg->n_kv_heads;
   a.n_q_heads = cfg->n_q_heads;
   a.n_rep = n_rep_of(cfg);
+  a.per_rep = (0x80000000u + (uint32_t)a.n_rep - 1) / (uint32_t)a.n_rep;
   a.n_tokens = n_tokens;
   a.max_new = std::min(max_new, n_tokens);
   a.kv_cap = INT32_MAX;
@@ -662,7 +663,6 @@ int fier_chunk_attn(const fier_config* cfg, const fier_cache* cache, const void*
   a.seq_lens = cache->seq_lens;
   a.lay = layout_of(cfg, cache);
   a.kv_cap = cfg->max_ctx;
-  a.from_cache = true;
   const Workspace w = carve(cfg, 1, workspace);
   a.counters = w.sb.hist;
   a.side_partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.zero_bytes);

@@ -222,7 +222,7 @@ struct PromptSpan {
   int first;  // rows in front of them that they attend over too
 };
 struct PromptArgs {  // attention of the new tokens (passed to the kernel by value)
-  const char *q, *k, *v;  // k, v: a cache's arrays if from_cache, else packed rows of the new tokens
+  const char *q, *k, *v;  // k, v: a cache's arrays if seq_lens, else packed rows of the new tokens
   char* out;
   int64_t q_stride, k_stride, v_stride;  // bytes from a token to the next (cache: from a row to the next)
   const int32_t *starts, *seq_lens;      // seq_lens: nullptr without a cache
@@ -233,8 +233,10 @@ struct PromptArgs {  // attention of the new tokens (passed to the kernel by val
   int n_tokens, max_new, kv_cap;  // kv_cap: rows of a cache; no limit without one
   float *side_partials, *shared_partials;
   uint32_t* counters;  // kSelBins words per unit, zero between calls
-  int side_grid, side_parts, shared_parts, side_slots, shared_slots;  // from PromptSplit
-  bool from_cache;
+  int side_items, side_parts, shared_parts, side_slots, shared_slots;  // from PromptSplit
+  uint32_t per_rep;  // ceil(2^31 / n_rep)
+  // row / n_rep for rows below 2^27: the quotient's error, row * (per_rep n_rep - 2^31) < 2^27 * 8, stays below 2^31
+  __device__ __forceinline__ int token_of(int row) const { return (int)__umulhi(2u * (uint32_t)row, per_rep); }
   // Whatever the offsets hold, the span lies inside the n_tokens rows.
   __device__ __forceinline__ PromptSpan span(int b) const {
     const int lo = max(0, min(starts[b], n_tokens)), hi = max(lo, min(starts[b + 1], n_tokens));
@@ -248,7 +250,7 @@ struct PromptArgs {  // attention of the new tokens (passed to the kernel by val
   }
 };
 struct PromptSplit {  // how the launch is cut
-  int64_t side_grid, shared_grid;     // workgroups
+  int64_t side_items, shared_items;   // workgroups per kv head
   int side_parts, shared_parts;       // parts of K / V rows wanted per kv head; 0: nothing is split
   int side_slots, shared_slots;       // partial results per kv head
   size_t side_floats, shared_floats;  // of all of them

@@ -6,6 +6,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "fier.h"
 #include "fier_dev.h"
@@ -39,10 +40,12 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2_t));
 }
 
+// The larger of two, a NaN if one is (one instruction; fmaxf has to quiet its operands first).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float halves_max(float x) {
   typedef unsigned int u2_t __attribute__((ext_vector_type(2)));
   const u2_t a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  return larger(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 __device__ __forceinline__ float halves_sum(float x) {
   typedef unsigned int u2_t __attribute__((ext_vector_type(2)));
@@ -76,9 +79,17 @@ __device__ __forceinline__ uint2 lds_read_transposed(const lds_char* p) {
 // Written as assembly, with a wait count of its own (wait_loads): the compiler takes every read of LDS for one that may need the
 // loads just issued, and waited for the next tile's rows before this one's product.  Nothing is returned in a register.  The
 // instruction after a write of M0 may not use it yet.
+// STREAM: with the hint for data that is read once.
+template <bool STREAM>
 __device__ __forceinline__ void load_rows_to_lds(const char* base, uint32_t off, const lds_char* dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)dst), "v"(off), "s"(base)
-               : "memory");
+  if (STREAM)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"((uint32_t)(uintptr_t)dst), "v"(off),
+                 "s"(base)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)dst), "v"(off),
+                 "s"(base)
+                 : "memory");
 }
 // until at most N of the wavefront's loads are under way
 template <int N>
@@ -90,8 +101,16 @@ __device__ __forceinline__ void meet() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// The lane's number anew: what is only needed after a loop need not live in registers through it.
+__device__ __forceinline__ int lane_again() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
 // The unit's K / V rows: row t of packed prompts, or of a cache, lies at row (t's block) * block_stride + (t & mask) of k and v.
 // Tiles of 32 or 64 rows start at multiples of their size, so that they lie inside a block.
+template <bool CACHE>
 struct UnitRows {
   const char *k, *v;
   int64_t k_stride, v_stride;  // bytes
@@ -101,8 +120,9 @@ struct UnitRows {
   size_t block_stride;
   int shift, mask;
   __device__ __forceinline__ UnitRows(const PromptArgs& a, int unit, int head, int lo)
-      : k(a.k), v(a.v), k_stride(a.k_stride), v_stride(a.v_stride), blocks(nullptr), block_stride(0), shift(0), mask(-1) {
-    if (a.from_cache) {
+      : k(a.k), v(a.v), k_stride(CACHE ? kRowBytes : a.k_stride), v_stride(CACHE ? kRowBytes : a.v_stride), blocks(nullptr),
+        block_stride(0), shift(0), mask(-1) {
+    if (CACHE) {
       const KvRows c = a.lay.rows_of(unit);
       k += c.base * kRowBytes;
       v += c.base * kRowBytes;
@@ -115,8 +135,10 @@ struct UnitRows {
       v += (int64_t)lo * v_stride + head * kRowBytes;
     }
   }
-  __device__ __forceinline__ int block_of(int t) const { return blocks ? blocks[t >> shift] : 0; }
-  __device__ __forceinline__ size_t row(int block, int t) const { return (size_t)block * block_stride + (size_t)(t & mask); }
+  __device__ __forceinline__ int block_of(int t) const { return CACHE && blocks ? blocks[t >> shift] : 0; }
+  __device__ __forceinline__ size_t row(int block, int t) const {
+    return CACHE ? (size_t)block * block_stride + (size_t)(t & mask) : (size_t)t;
+  }
 };
 
 // A wavefront's share of a tile: N instructions, rows 4 (n0 + STEP j) .. + 3 of instruction j.  The permutation of a row's chunks
@@ -136,18 +158,47 @@ struct RowLoads {
       off[j] = (uint32_t)row * (uint32_t)stride + chunk(row, lane);
     }
   }
-  // rows: how many the tile has; the others take the last one's (they get no weight)
-  __device__ __forceinline__ void load(const char* src, int64_t stride, int rows, const lds_char* dst, int n0, int lane) const {
-    if (rows >= 4 * N * STEP) {
+  template <bool STREAM>
+  __device__ __forceinline__ void load_whole(const char* src, int64_t stride, const lds_char* dst, int n0) const {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        load_rows_to_lds(src + (int64_t)(4 * STEP * (j / kCycle * kCycle)) * stride, off[j % kCycle], dst + 4 * (n0 + STEP * j) * kRowBytes);
+    for (int j = 0; j < N; ++j)
+      load_rows_to_lds<STREAM>(src + (int64_t)(4 * STEP * (j / kCycle * kCycle)) * stride, off[j % kCycle],
+                               dst + 4 * (n0 + STEP * j) * kRowBytes);
+  }
+  // rows: how many the tile has; the others take the last one's (they get no weight)
+  __device__ __forceinline__ void load(const char* src, int64_t stride, int rows, const lds_char* dst, int n0,
+                                       bool stream = false) const {
+    if (rows >= 4 * N * STEP) {
+      if (stream) load_whole<true>(src, stride, dst, n0);
+      else load_whole<false>(src, stride, dst, n0);
     } else {
+      const int lane = lane_again();
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const int row = 4 * (n0 + STEP * j) + (lane >> 4);
-        load_rows_to_lds(src, (uint32_t)min(row, rows - 1) * (uint32_t)stride + chunk(row, lane), dst + 4 * (n0 + STEP * j) * kRowBytes);
+        load_rows_to_lds<false>(src, (uint32_t)min(row, rows - 1) * (uint32_t)stride + chunk(row, lane),
+                                dst + 4 * (n0 + STEP * j) * kRowBytes);
       }
+    }
+  }
+};
+
+// The lane's places in a K and a V tile of 32 rows, in registers: what differs from read to read is then a constant offset.
+struct LdsReads {
+  const lds_char *k[8], *v[4];
+  __device__ __forceinline__ LdsReads(const lds_char* kt, const lds_char* vt, int lane) {
+    const int n = lane & 31, h = lane >> 5, r4 = (lane & 15) >> 2, g1 = (lane >> 4) & 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t at = (uint32_t)(uintptr_t)kt + n * kRowBytes + (((2 * i + h) ^ (n & 15)) << 4);
+      asm("" : "+v"(at));  // not made anew from its parts each time
+      k[i] = (const lds_char*)(uintptr_t)at;
+    }
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) {
+      uint32_t at = (uint32_t)(uintptr_t)vt + (4 * h + r4) * kRowBytes + (lane & 3) * 8 + (((2 * ct + g1) ^ (2 * r4 + h)) << 5);
+      asm("" : "+v"(at));
+      v[ct] = (const lds_char*)(uintptr_t)at;
     }
   }
 };
@@ -172,15 +223,14 @@ struct Rows32 {
     large = false;
   }
 
+  // at: bytes from the tiles that `r` was made for
   template <int M>
-  __device__ __forceinline__ static void scores(const lds_char* kt, const uint4 (&q)[8], int n, int h, floatx16_t (&s)[M]) {
-    const lds_char* const kr = kt + n * kRowBytes;
+  __device__ __forceinline__ static void scores(const LdsReads& r, int at, const uint4 (&q)[8], floatx16_t (&s)[M]) {
 #pragma unroll
     for (int mt = 0; mt < M; ++mt) {
       s[mt] = floatx16_t{0.f};
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        s[mt] = mfma_32x32x16<DT>(lds_read16(kr + mt * 32 * kRowBytes + (((2 * k + h) ^ (n & 15)) << 4)), q[k], s[mt]);
+      for (int k = 0; k < 8; ++k) s[mt] = mfma_32x32x16<DT>(lds_read16(r.k[k] + (at + mt * 32 * kRowBytes)), q[k], s[mt]);
     }
   }
 
@@ -196,7 +246,7 @@ struct Rows32 {
     }
     float mx = s[0][0];
 #pragma unroll
-    for (int i = 1; i < 16 * M; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
+    for (int i = 1; i < 16 * M; ++i) mx = larger(mx, s[i >> 4][i & 15]);
     mx = halves_max(mx);
     const float top = rounded_product(mx, c) - kBias;
     if (__any(top > (large ? m : m + kSlack))) {
@@ -221,9 +271,7 @@ struct Rows32 {
   }
 
   template <int M>
-  __device__ __forceinline__ void add_values(const lds_char* vt, const floatx16_t (&p)[M], int lane, int h) {
-    const int r4 = (lane & 15) >> 2, g1 = (lane >> 4) & 1;
-    const lds_char* const vr = vt + (4 * h + r4) * kRowBytes + (lane & 3) * 8;
+  __device__ __forceinline__ void add_values(const LdsReads& r, int at, const floatx16_t (&p)[M]) {
 #pragma unroll
     for (int t = 0; t < 2 * M; ++t) {
       const int i = 8 * (t & 1);
@@ -232,8 +280,8 @@ struct Rows32 {
                                   pack2<DT>(x[i + 6], x[i + 7]));
 #pragma unroll
       for (int ct = 0; ct < 4; ++ct) {
-        const lds_char* const at = vr + t * 16 * kRowBytes + (((2 * ct + g1) ^ (2 * r4 + h)) << 5);
-        const uint2 v0 = lds_read_transposed(at), v1 = lds_read_transposed(at + 8 * kRowBytes);
+        const lds_char* const from = r.v[ct] + (at + t * 16 * kRowBytes);
+        const uint2 v0 = lds_read_transposed(from), v1 = lds_read_transposed(from + 8 * kRowBytes);
         o[ct] = mfma_32x32x16<DT>(make_uint4(v0.x, v0.y, v1.x, v1.y), pb, o[ct]);
       }
     }
@@ -248,13 +296,6 @@ __device__ __forceinline__ void store_channels(char* out_row, int ct, int h, con
         make_uint2(pack2<DT>(o[4 * i] * inv, o[4 * i + 1] * inv), pack2<DT>(o[4 * i + 2] * inv, o[4 * i + 3] * inv));
 }
 
-// The lane's number anew: what is only needed after a loop need not live in registers through it.
-__device__ __forceinline__ int lane_again() {
-  int l;
-  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
-  return l;
-}
-
 // ---- one query row per lane and half ------------------------------------------------------------------------------------
 struct QueryRow {
   const char* q;
@@ -264,7 +305,7 @@ struct QueryRow {
   __device__ __forceinline__ QueryRow(const PromptArgs& a, const PromptSpan& sp, int head, int row, int n_rows) {
     there = row < n_rows;
     row = there ? row : n_rows - 1;
-    const int tok = row / a.n_rep, qh = head * a.n_rep + row - tok * a.n_rep;
+    const int tok = a.token_of(row), qh = head * a.n_rep + row - tok * a.n_rep;
     lim = min(sp.first + tok + 1, a.kv_cap);
     q = a.q + (size_t)(sp.lo + tok) * a.q_stride + qh * kRowBytes;
     out = a.out + ((size_t)(sp.lo + tok) * a.n_q_heads + qh) * kRowBytes;
@@ -289,9 +330,8 @@ __device__ __forceinline__ void store_partial_sums(float* slot, float m, float l
 // Channel tiles ct0 .. ct0 + CT - 1 of n slots, `pitch` floats apart, joined; BATCH slots' loads are under way together.
 template <int CT, int BATCH>
 __device__ __forceinline__ void join_partials(const float* slots, size_t pitch, int n, int ct0, int lane, floatx16_t (&o)[CT],
-                                              float& l) {
-  float m = -FLT_MAX;
-  l = 0.f;
+                                              float& m, float& l) {
+  m = -FLT_MAX, l = 0.f;
 #pragma unroll
   for (int c = 0; c < CT; ++c) o[c] = floatx16_t{0.f};
   for (int p0 = 0; p0 < n; p0 += BATCH) {
@@ -332,12 +372,21 @@ __device__ __forceinline__ void join_partials(const float* slots, size_t pitch, 
 constexpr int kSideTile = 32;    // rows of K and V per wavefront and step where the wavefronts go side by side
 constexpr int kSideWaves = 3;    // of four: three such workgroups fit a CU's LDS
 constexpr int kSideStep = kSideWaves * kSideTile;
-#ifndef MAXP
-#define MAXP 48
+#ifndef SIDEL
+#define SIDEL 2
 #endif
-constexpr int kMostParts = MAXP;  // of a tile
-constexpr int kSideLeast = 2;    // steps of a part there, at least
-constexpr int kSharedLeast = 8;  // steps of 64 rows of a part where the wavefronts share the tiles, at least
+#ifndef SHAREDL
+#define SHAREDL 8
+#endif
+constexpr int kSideLeast = SIDEL;    // steps of a part there, at least
+constexpr int kSharedLeast = SHAREDL;  // steps of 64 rows of a part where the wavefronts share the tiles, at least
+// Parts of a tile: up to 8 are joined by the last of its workgroups; more by the last of every group of 7 or fewer, and the groups
+// by the last of them (one workgroup reads 3 MB of 48 parts of 128 rows in 25 us, meanwhile nobody else has work).  A tile's
+// counters: one for the whole and one for each group; a sequence of more tiles than there is room for has up to 8 parts, and
+// one of more still is not split.
+constexpr int kGroup = 8, kMostParts = 48;
+constexpr float kStreamBytes = 64 << 20;  // K and V rows from here on take the streaming hint (side by side)
+constexpr unsigned kGridY = 32768;  // items along y, the rest along z
 
 // ---- which workgroup does what -----------------------------------------------------------------------------------------------
 // A sequence's query rows per kv head are cut into tiles of 128; the last one, where it has at most 32, goes through its K / V
@@ -371,11 +420,7 @@ struct SequenceWork {
   template <bool SIDE>
   __device__ __forceinline__ int parts(int step) const {  // that its tiles have at most; more tiles than counters: not split
     const int n = steps<SIDE>();
-    return n <= step || (!SIDE && tiles >= kSelBins - 1) ? 1 : min((n + step - 1) / step, kMostParts);
-  }
-  template <bool SIDE>
-  __device__ __forceinline__ int items(int step) const {
-    return SIDE ? (aside ? parts<true>(step) : 0) : tiles * parts<false>(step);
+    return n <= step ? 1 : min((n + step - 1) / step, SIDE && n <= kGroup * kGroup ? kGroup : kMostParts);
   }
 };
 struct Item {
@@ -384,6 +429,7 @@ struct Item {
   int parts;    // of its tiles
   int step;     // steps of a part
   int slot;     // partial results: the place of the sequence's first item
+  bool stream;  // K and V are loaded with the streaming hint
 };
 // Sum of the lanes' values, the same in every lane and workgroup.
 __device__ __forceinline__ float wave_sum_ordered(float x) {
@@ -392,28 +438,38 @@ __device__ __forceinline__ float wave_sum_ordered(float x) {
   return (__int_as_float(__builtin_amdgcn_readlane(v, 0)) + __int_as_float(__builtin_amdgcn_readlane(v, 16))) +
          (__int_as_float(__builtin_amdgcn_readlane(v, 32)) + __int_as_float(__builtin_amdgcn_readlane(v, 48)));
 }
+// Where part p of n begins: all <= 2^14 steps, p <= n <= 48.
+__device__ __forceinline__ int part_begin(int all, int p, int n) { return (int)((unsigned)(all * p) / (unsigned)n); }
 // Item number j of the launch's (per kv head); false: there are fewer.
-template <bool SIDE>
+template <bool SIDE, bool SPLIT>
 __device__ __forceinline__ bool find_item(const PromptArgs& a, int j, int lane, Item& it) {
-  const int wanted = SIDE ? a.side_parts : a.shared_parts;  // 0: nothing is split
+  int64_t tokens0 = 0;
+  const SequenceWork w0(a, lane, lane, tokens0);  // more than 64 sequences: the others are looked at in turn
   it.step = 1 << 30;
-  if (wanted) {
-    float all = 0.f;
-    int64_t tokens = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 64) {
-      const SequenceWork w(a, b0 + lane, lane, tokens);
-      all += wave_sum_ordered((float)(SIDE ? (w.aside ? 1 : 0) : w.tiles) * (float)w.steps<SIDE>());
-    }
-    it.step = max(SIDE ? kSideLeast : kSharedLeast, (int)ceilf(all / (float)wanted));
-    it.step = __builtin_amdgcn_readfirstlane(it.step);
+  it.stream = false;
+  if (SPLIT) {
+    // steps of all tiles, and (shared) tiles
+    float all = 0.f, tiles = 0.f;
+    auto count = [&](const SequenceWork& w) {
+      const float n = (float)(SIDE ? (w.aside ? 1 : 0) : w.tiles);
+      all += wave_sum_ordered(n * (float)w.steps<SIDE>());
+      if (!SIDE) tiles += wave_sum_ordered(n);
+    };
+    count(w0);
+    int64_t tokens = tokens0;
+    for (int b0 = 64; b0 < a.batch; b0 += 64) count(SequenceWork(a, b0 + lane, lane, tokens));
+    // A tile of s steps becomes ceil(s / step) items, half of one more than s / step on average.
+    const float parts = (float)(SIDE ? a.side_parts : a.shared_parts);
+    const float wanted = SIDE || tiles > 1.2f * parts ? (SIDE ? 1.f : 2.f) * parts : (tiles > 0.6f * parts ? 2.f : 1.f) * parts - 0.5f * tiles;
+    it.step = __builtin_amdgcn_readfirstlane(max(SIDE ? kSideLeast : kSharedLeast, (int)ceilf(all / wanted)));
+    it.stream = all * (float)a.n_kv_heads * (2.f * kSideStep * kRowBytes) >= kStreamBytes;
   }
   int before = 0, slots = 0;
-  int64_t tokens = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const SequenceWork w(a, b0 + lane, lane, tokens);
-    const int parts = w.parts<SIDE>(it.step), n = w.items<SIDE>(it.step), split = parts > 1 ? n : 0;
+  auto look = [&](const SequenceWork& w, int b0) {
+    const int parts = SPLIT ? w.parts<SIDE>(it.step) : 1, n = (SIDE ? (w.aside ? 1 : 0) : w.tiles) * parts;
+    const int split = parts > 1 ? n : 0;
     const int upto = before + (int)wave_incl_scan_u32((uint32_t)n, lane);
-    const int slots_upto = slots + (int)wave_incl_scan_u32((uint32_t)split, lane);
+    const int slots_upto = SPLIT ? slots + (int)wave_incl_scan_u32((uint32_t)split, lane) : 0;
     const unsigned long long past = __ballot(upto > j);
     if (past) {
       const int l = __builtin_ctzll(past);
@@ -426,13 +482,47 @@ __device__ __forceinline__ bool find_item(const PromptArgs& a, int j, int lane, 
     }
     before = __builtin_amdgcn_readlane(upto, 63);
     slots = __builtin_amdgcn_readlane(slots_upto, 63);
-  }
+    return false;
+  };
+  if (look(w0, 0)) return true;
+  for (int b0 = 64; b0 < a.batch; b0 += 64)
+    if (look(SequenceWork(a, b0 + lane, lane, tokens0), b0)) return true;
   return false;
 }
 
+// One part of n_parts is done: its partial results (channel tiles ct0 .. ct0 + CT - 1 of the wavefront's lanes that are there) go
+// to its slot, and the last workgroup of all returns true with those of all parts joined in o, m and l.
+template <int CT, int BATCH>
+__device__ __forceinline__ bool join_parts(float* slots, size_t pitch, int n_parts, int part, uint32_t* counters, bool there, int ct0,
+                                           bool sums, int wave, int lane, floatx16_t (&o)[CT], float& m, float& l, uint32_t* flag) {
+  const bool first = wave == 0 && lane == 0;
+  auto put = [&](int at) {
+    if (!there) return;
+    float* const slot = slots + (size_t)at * pitch;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) store_partial(slot, ct0 + c, o[c], lane);
+    if (sums) store_partial_sums(slot, m, l, lane);
+  };
+  put(part);
+  int group = 1, n = n_parts;  // parts per group, groups
+  if (n_parts > kGroup) {
+    group = 3;
+    while (group * group < n_parts) ++group;  // at most 7
+    n = (n_parts + group - 1) / group;
+    const int g = part / group, size = min(group, n_parts - g * group);
+    if (arrive_add(counters + 1 + g, 1u, flag, first) != (uint32_t)size - 1) return false;
+    if (there) join_partials<CT, BATCH>(slots + (size_t)(g * group) * pitch, pitch, size, ct0, lane, o, m, l);
+    if (first) store_coherent(counters + 1 + g, 0u);
+    put(g * group);
+  }
+  if (arrive_add(counters, 1u, flag, first) != (uint32_t)n - 1) return false;
+  if (there) join_partials<CT, BATCH>(slots, pitch * group, n, ct0, lane, o, m, l);
+  if (first) store_coherent(counters, 0u);
+  return true;
+}
 
 // The wavefronts' results of a side-by-side tile: each puts its own into its LDS, then takes one channel tile of all.
-template <int DT>
+template <int DT, bool CACHE>
 __device__ __forceinline__ void join_side_by_side(const PromptArgs& a, const Item& it, int head, const Rows32<DT>& st, int wave,
                                                   lds_char* lds, uint32_t* flag) {
   const int lane = lane_again(), h = lane >> 5;
@@ -468,37 +558,31 @@ __device__ __forceinline__ void join_side_by_side(const PromptArgs& a, const Ite
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[0][i] += f * p[(wave * 16 + i) * 64 + lane];
   }
-  if (n_parts > 1) {
-    float* const slots = a.side_partials + ((size_t)head * a.side_slots + it.slot) * kPartFloats;
-    if (row.there) {
-      store_partial(slots + (size_t)part * kPartFloats, wave, o[0], lane);
-      if (wave == 0) store_partial_sums(slots + (size_t)part * kPartFloats, m, sum, lane);
-    }
-    uint32_t* const counter = a.counters + (size_t)unit * kSelBins;
-    if (arrive_add(counter, 1u, flag, wave == 0 && lane == 0) != (uint32_t)n_parts - 1) return;  // not the last one
-    if (row.there) join_partials<1, 8>(slots, kPartFloats, n_parts, wave, lane, o, sum);
-    if (wave == 0 && lane == 0) store_coherent(counter, 0u);
-  }
+  if (CACHE && n_parts > 1 && !join_parts<1, 8>(a.side_partials + ((size_t)head * a.side_slots + it.slot) * kPartFloats, kPartFloats, n_parts,
+                                       part, a.counters + (size_t)unit * kSelBins, row.there, wave, wave == 0, wave, lane, o, m,
+                                       sum, flag))
+    return;
   if (row.there) store_channels<DT>(row.out, wave, h, o[0], sum > 0.f ? 1.f / sum : 0.f);
 }
 
 // Up to 32 query rows: all four wavefronts hold them and go side by side through the K / V rows, each through 32 of every 128,
 // in 16 KiB of LDS of its own, so that nobody waits for anybody.  The next K rows are loaded once this step's logits are
 // there, the next V rows after its product.  Bound by memory.
-template <int DT>
+template <int DT, bool CACHE>
 __device__ __forceinline__ void attend_side_by_side(const PromptArgs& a, const Item& it, int head, lds_char* lds, uint32_t* flag) {
   const PromptSpan sp = it.sp;
   const int unit = it.b * a.n_kv_heads + head, n_rows = sp.n * a.n_rep, row0 = n_rows / kRowTile * kRowTile;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
-  const int n_kv = min(sp.first + (n_rows - 1) / a.n_rep + 1, a.kv_cap);
+  const int n_kv = min(sp.first + sp.n, a.kv_cap);
   const int all = (n_kv + kSideStep - 1) / kSideStep, n_parts = it.parts;
-  const int begin = (int)((int64_t)all * it.at / n_parts), end = (int)((int64_t)all * (it.at + 1) / n_parts);
+  const int begin = CACHE ? part_begin(all, it.at, n_parts) : 0, end = CACHE ? part_begin(all, it.at + 1, n_parts) : all;
   const QueryRow row(a, sp, head, row0 + n, n_rows);
   const int least = __builtin_amdgcn_readfirstlane(row.lim);  // the first row's
-  const UnitRows rows(a, unit, head, sp.lo);
+  const UnitRows<CACHE> rows(a, unit, head, sp.lo);
   lds_char* const kt = lds + wave * 2 * kSideTile * kRowBytes;
   lds_char* const vt = kt + kSideTile * kRowBytes;
+  const LdsReads reads(kt, vt, lane);
   const RowLoads<false, 8, 1> kl(0, lane, rows.k_stride);
   const RowLoads<true, 8, 1> vl(0, lane, rows.v_stride);
   int t0 = begin * kSideStep + wave * kSideTile;
@@ -506,8 +590,8 @@ __device__ __forceinline__ void attend_side_by_side(const PromptArgs& a, const I
   int block = 0;
   if (t0 < stop) {
     const size_t r = rows.row(rows.block_of(t0), t0);
-    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - t0, kt, 0, lane);
-    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - t0, vt, 0, lane);
+    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - t0, kt, 0, it.stream);
+    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - t0, vt, 0, it.stream);
     block = rows.block_of(t0 + kSideStep < stop ? t0 + kSideStep : t0);
   }
   uint4 q[8];
@@ -520,69 +604,141 @@ __device__ __forceinline__ void attend_side_by_side(const PromptArgs& a, const I
     const size_t r = rows.row(block, next);
     floatx16_t s[1];
     wait_loads<8>();
-    Rows32<DT>::scores(kt, q, n, h, s);
+    Rows32<DT>::scores(reads, 0, q, s);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, kt, 0, lane);
+    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, kt, 0, it.stream);
     block = rows.block_of(next + kSideStep < stop ? next + kSideStep : next);  // for the step after the next: the list is far away
     st.weights(s, a.scale, t0 + kSideTile > least, row.lim - t0, h);
     wait_loads<8>();
-    st.add_values(vt, s, lane, h);
+    st.add_values(reads, 0, s);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - next, vt, 0, lane);
+    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - next, vt, 0, it.stream);
   }
   wait_loads<0>();
-  join_side_by_side<DT>(a, it, head, st, wave, lds, flag);
+  join_side_by_side<DT, CACHE>(a, it, head, st, wave, lds, flag);
 }
-// The results of a tile of shared rows, through partial results where its K / V rows were split.
-template <int DT>
-__device__ __forceinline__ void finish_shared(const PromptArgs& a, const Item& it, int head, int tile, int turned, int part, int n_parts,
-                                              Rows32<DT>& st, int wave, uint32_t* flag) {
-  const int lane = lane_again(), h = lane >> 5;
-  const int unit = it.b * a.n_kv_heads + head;
-  const QueryRow row(a, it.sp, head, tile * kRowTile + wave * 32 + (lane & 31), it.sp.n * a.n_rep);
-  float l = halves_sum(st.l);
-  if (n_parts > 1) {
-    float* const slots = a.shared_partials + (((size_t)head * a.shared_slots + it.slot + turned * it.parts) * 4 + wave) * kPartFloats;
-    if (row.there) {
-      float* const slot = slots + (size_t)part * 4 * kPartFloats;
-#pragma unroll
-      for (int ct = 0; ct < 4; ++ct) store_partial(slot, ct, st.o[ct], lane);
-      store_partial_sums(slot, st.m, l, lane);
-    }
-    uint32_t* const counter = a.counters + (size_t)unit * kSelBins + 1 + tile;
-    if (arrive_add(counter, 1u, flag, wave == 0 && lane == 0) != (uint32_t)n_parts - 1) return;  // not the last one
-    if (row.there) join_partials<4, 2>(slots, 4 * kPartFloats, n_parts, 0, lane, st.o, l);
-    if (wave == 0 && lane == 0) store_coherent(counter, 0u);
+// Which tile and part of a sequence's shared rows an item is; the tiles that attend over the most rows come first.
+struct SharedTile {
+  int tiles, turned, tile, part, n_kv, all, n_parts;  // n_kv rows, `all` steps; a prompt's first tiles have fewer than the last
+  __device__ __forceinline__ SharedTile(const PromptArgs& a, const Item& it) {
+    const int n_rows = it.sp.n * a.n_rep;
+    tiles = n_rows / kRowTile + (n_rows % kRowTile > kSideRows ? 1 : 0);
+    turned = it.parts > 1 ? it.at / it.parts : it.at;
+    part = it.at - turned * it.parts;
+    tile = tiles - 1 - turned;
+    n_kv = min(it.sp.first + a.token_of(min((tile + 1) * kRowTile, n_rows) - 1) + 1, a.kv_cap);
+    all = (n_kv + kTile - 1) / kTile;
+    n_parts = it.parts > 1 ? min(it.parts, (all + it.step - 1) / it.step) : 1;
   }
+};
+
+// ---- shared tiles in several parts: a second launch joins them ------------------------------------------------------------------
+// Per wavefront o as the lanes hold it, 16 chunks of 64 x 4 floats (channel tile ct, channels 8 i + 4 h + 0..3: chunk 4 ct + i),
+// then m and l of the lanes.
+__device__ __forceinline__ float* shared_slot(const PromptArgs& a, const Item& it, int head, int turned, int part) {
+  return a.shared_partials + ((size_t)head * a.shared_slots + it.slot + turned * it.parts + part) * (4 * kPartFloats);
+}
+template <int DT, bool CACHE>
+__device__ __forceinline__ void finish_shared(const PromptArgs& a, const Item& it, int head, int tiles, int turned, int part, int n_parts,
+                                              const Rows32<DT>& st, int wave) {
+  const int lane = lane_again(), h = lane >> 5;
+  const float l = halves_sum(st.l);
+  if (CACHE && n_parts > 1) {
+    float4* const p = reinterpret_cast<float4*>(shared_slot(a, it, head, turned, part) + wave * kPartFloats) + lane;
+#pragma unroll
+    for (int c = 0; c < 16; ++c)
+      p[c * 64] = make_float4(st.o[c >> 2][4 * (c & 3)], st.o[c >> 2][4 * (c & 3) + 1], st.o[c >> 2][4 * (c & 3) + 2], st.o[c >> 2][4 * (c & 3) + 3]);
+    reinterpret_cast<float2*>(p - lane + 16 * 64)[lane] = make_float2(st.m, l);
+    return;
+  }
+  const QueryRow row(a, it.sp, head, (tiles - 1 - turned) * kRowTile + wave * 32 + (lane & 31), it.sp.n * a.n_rep);
   if (!row.there) return;
   const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct) store_channels<DT>(row.out, ct, h, st.o[ct], inv);
 }
 
-// 128 query rows, 32 a wavefront; the K / V rows go through LDS 64 at a time, two tiles of each, shared by the wavefronts.
+// CH chunks of a wavefront's 32 rows at a time, BATCH parts' loads under way together.
+template <int DT, int CH, int BATCH>
+__device__ __forceinline__ void join_chunks(const PromptArgs& a, const Item& it, int head, const SharedTile& t, int first, int lane) {
+  for (int c = first * CH; c < 64; c += 4 * CH * t.n_parts) {
+    const float* const from = shared_slot(a, it, head, t.turned, 0) + (c >> 4) * kPartFloats;
+    float m = -FLT_MAX, l = 0.f, o[CH][4] = {};
+    for (int p0 = 0; p0 < t.n_parts; p0 += BATCH) {
+      float4 w[BATCH][CH];
+      float2 ml[BATCH];
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const float4* const slot = reinterpret_cast<const float4*>(from + (size_t)min(p0 + k, t.n_parts - 1) * (4 * kPartFloats));
+#pragma unroll
+        for (int x = 0; x < CH; ++x) w[k][x] = slot[((c & 15) + x) * 64 + lane];
+        ml[k] = reinterpret_cast<const float2*>(slot + 16 * 64)[lane];
+      }
+      float to = m;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) to = fmaxf(to, ml[k].x);
+      const float alpha = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= alpha;
+#pragma unroll
+      for (int x = 0; x < CH; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[x][i] *= alpha;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const float f = p0 + k < t.n_parts ? __builtin_amdgcn_exp2f(ml[k].x - m) : 0.f;
+        l += f * ml[k].y;
+#pragma unroll
+        for (int x = 0; x < CH; ++x)
+          o[x][0] += f * w[k][x].x, o[x][1] += f * w[k][x].y, o[x][2] += f * w[k][x].z, o[x][3] += f * w[k][x].w;
+      }
+    }
+    const QueryRow row(a, it.sp, head, t.tile * kRowTile + (c >> 4) * 32 + (lane & 31), it.sp.n * a.n_rep);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    if (row.there) {
+#pragma unroll
+      for (int x = 0; x < CH; ++x)
+        *reinterpret_cast<uint2*>(row.out + ((c & 15) + x) * 16 + (lane >> 5) * 8) =
+            make_uint2(pack2<DT>(o[x][0] * inv, o[x][1] * inv), pack2<DT>(o[x][2] * inv, o[x][3] * inv));
+    }
+  }
+}
+// One workgroup for every part of the first launch; a tile's share the 64 chunks of its rows.
 template <int DT>
-__device__ __forceinline__ void attend_shared(const PromptArgs& a, const Item& it, int head, lds_char* lds, uint32_t* flag) {
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = (int)(blockIdx.z * kGridY + blockIdx.y), head = (int)blockIdx.x;
+  Item it;
+  if (!find_item<false, true>(a, j, lane, it) || it.parts == 1) return;
+  const SharedTile t(a, it);
+  if (t.part >= t.n_parts || t.n_parts == 1) return;
+  // The fewer the parts, the more chunks a wavefront has: 16 loads under way in any case.
+  const int first = t.part * 4 + wave;
+  if (t.n_parts <= 2) join_chunks<DT, 8, 2>(a, it, head, t, first, lane);
+  else if (t.n_parts <= 4) join_chunks<DT, 4, 4>(a, it, head, t, first, lane);
+  else if (t.n_parts <= 8) join_chunks<DT, 2, 8>(a, it, head, t, first, lane);
+  else join_chunks<DT, 1, 16>(a, it, head, t, first, lane);
+}
+
+// 128 query rows, 32 a wavefront; the K / V rows go through LDS 64 at a time, two tiles of each, shared by the wavefronts.
+template <int DT, bool CACHE>
+__device__ __forceinline__ void attend_shared(const PromptArgs& a, const Item& it, int head, lds_char* lds) {
   const PromptSpan sp = it.sp;
   const int unit = it.b * a.n_kv_heads + head, n_rows = sp.n * a.n_rep;
-  const int tiles = n_rows / kRowTile + (n_rows % kRowTile > kSideRows ? 1 : 0);
-  // the tiles that attend over the most rows first
-  const int turned = it.at / it.parts, tile = tiles - 1 - turned, part = it.at - turned * it.parts;
+  const SharedTile t(a, it);
+  const int part = t.part, n_parts = t.n_parts, n_kv = t.n_kv, all = t.all, row0 = t.tile * kRowTile;
+  if (CACHE && part >= n_parts) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
-  const int row0 = tile * kRowTile;
-  const int n_kv = min(sp.first + (min(row0 + kRowTile, n_rows) - 1) / a.n_rep + 1, a.kv_cap);
-  const int all = (n_kv + kTile - 1) / kTile, n_parts = min(it.parts, (all + it.step - 1) / it.step);
-  if (part >= n_parts) return;  // the first tiles of a prompt attend over fewer rows than the last one
-  const int begin = (int)((int64_t)all * part / n_parts), end = (int)((int64_t)all * (part + 1) / n_parts);
+  const int begin = CACHE ? part_begin(all, part, n_parts) : 0, end = CACHE ? part_begin(all, part + 1, n_parts) : all;
   const QueryRow row(a, sp, head, row0 + wave * 32 + n, n_rows);
   const int least = __builtin_amdgcn_readfirstlane(row.lim), most = __builtin_amdgcn_readlane(row.lim, 31);
-  const UnitRows rows(a, unit, head, sp.lo);
+  const UnitRows<CACHE> rows(a, unit, head, sp.lo);
   constexpr int kBytes = kTile * kRowBytes;
   const RowLoads<false, 4, 4> kl(wave, lane, rows.k_stride);
   const RowLoads<true, 4, 4> vl(wave, lane, rows.v_stride);
   const size_t r0 = rows.row(rows.block_of(begin * kTile), begin * kTile);
-  kl.load(rows.k + r0 * rows.k_stride, rows.k_stride, n_kv - begin * kTile, lds, wave, lane);
+  kl.load(rows.k + r0 * rows.k_stride, rows.k_stride, n_kv - begin * kTile, lds, wave);
   size_t r = r0;
   int block = rows.block_of(min(begin + 1, end - 1) * kTile);
   uint4 q[8];
@@ -591,54 +747,59 @@ __device__ __forceinline__ void attend_shared(const PromptArgs& a, const Item& i
   Rows32<DT> st;
   st.init();
   lds_char* const vt = lds + 2 * kBytes;
-  for (int i = begin; i < end; ++i) {
-    const int t0 = i * kTile, next = i + 1 < end ? t0 + kTile : t0, cur = (i - begin) & 1;
-    const lds_char* const kt = lds + cur * kBytes;
+  const LdsReads reads(lds, vt, lane);
+  // Tile i, its K rows in the buffer CUR: a constant, so that it goes into the reads' offsets.
+  auto step = [&](int i, auto CUR) {
+    constexpr int cur = decltype(CUR)::value;
+    const int t0 = i * kTile, next = i + 1 < end ? t0 + kTile : t0;
     wait_loads<0>();
     meet();
-    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - t0, vt, wave, lane);
+    vl.load(rows.v + r * rows.v_stride, rows.v_stride, n_kv - t0, vt, wave);
     r = rows.row(block, next);
-    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, lds + (cur ^ 1) * kBytes, wave, lane);
+    kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, lds + (cur ^ 1) * kBytes, wave);
     block = rows.block_of(min(i + 2, end - 1) * kTile);
     floatx16_t s[1];
     if (t0 < most) {  // some of the wavefront's rows go that far
-      Rows32<DT>::scores(kt, q, n, h, s);
+      Rows32<DT>::scores(reads, cur * kBytes, q, s);
       st.weights(s, a.scale, t0 + 32 > least, row.lim - t0, h);
     }
     wait_loads<4>();
     meet();
-    if (t0 < most) st.add_values(vt, s, lane, h);
+    if (t0 < most) st.add_values(reads, 0, s);
     if (t0 + 32 < most) {
-      Rows32<DT>::scores(kt + 32 * kRowBytes, q, n, h, s);
+      Rows32<DT>::scores(reads, cur * kBytes + 32 * kRowBytes, q, s);
       st.weights(s, a.scale, t0 + kTile > least, row.lim - t0 - 32, h);
-      st.add_values(vt + 32 * kRowBytes, s, lane, h);
+      st.add_values(reads, 32 * kRowBytes, s);
     }
+  };
+  for (int i = begin; i < end; i += 2) {
+    step(i, std::integral_constant<int, 0>());
+    if (i + 1 < end) step(i + 1, std::integral_constant<int, 1>());
   }
   wait_loads<0>();
-  finish_shared<DT>(a, it, head, tile, turned, part, n_parts, st, wave, flag);
+  finish_shared<DT, CACHE>(a, it, head, t.tiles, t.turned, part, n_parts, st, wave);
 }
 
 // The grid lists the side-by-side items first, then the shared ones, the kv heads of an item next to each other: with a multiple
 // of 8 of them a head's K and V stay in one XCD's L2.  What has no work leaves at once.  A tile whose K / V rows are split hands
 // its partial results to the last of its workgroups.
-template <int DT>
+//   CACHE: over a cache's rows, split where there are few tiles; else packed prompts, not split.
+template <int DT, bool CACHE>
 __global__ __launch_bounds__(256, 3) void prompt_attn_kernel(PromptArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[3 * kTile * kRowBytes + kSideWaves * 64 * 8];
   __shared__ uint32_t flag;
   const int lane = threadIdx.x & 63;
-  const bool side = blockIdx.x < (unsigned)a.side_grid;
-  const unsigned id = side ? blockIdx.x : blockIdx.x - (unsigned)a.side_grid;
-  const int j = (int)(id / (unsigned)a.n_kv_heads), head = (int)(id - (unsigned)j * (unsigned)a.n_kv_heads);
+  const int j = (int)(blockIdx.z * kGridY + blockIdx.y), head = (int)blockIdx.x;
   Item it;
-  if (side) {
-    if (find_item<true>(a, j, lane, it)) attend_side_by_side<DT>(a, it, head, (lds_char*)lds, &flag);
+  if (j < a.side_items) {
+    if (find_item<true, CACHE>(a, j, lane, it)) attend_side_by_side<DT, CACHE>(a, it, head, (lds_char*)lds, &flag);
   } else {
-    if (find_item<false>(a, j, lane, it)) attend_shared<DT>(a, it, head, (lds_char*)lds, &flag);
+    if (find_item<false, CACHE>(a, j - a.side_items, lane, it)) attend_shared<DT, CACHE>(a, it, head, (lds_char*)lds);
   }
 }
 
 #ifndef SIDE_T
-#define SIDE_T 1536
+#define SIDE_T 768
 #endif
 #ifndef SHARED_T
 #define SHARED_T 768
@@ -651,11 +812,13 @@ PromptSplit prompt_split(int batch, int n_kv_heads, int n_rep, int n_tokens, int
   const int64_t seqs = std::min(batch, n_tokens);
   sp.side_parts = split ? std::max(1, SIDE_T / n_kv_heads) : 0;
   sp.shared_parts = split && shared ? std::max(1, SHARED_T / n_kv_heads) : 0;
-  sp.side_grid = (seqs + sp.side_parts) * n_kv_heads;
-  sp.shared_grid = shared ? (all_rows / kRowTile + seqs + sp.shared_parts) * n_kv_heads : 0;
-  // Items of tiles in more than one part: at most twice the parts wanted, since ceil(x) < 2 x for x > 1.
-  sp.side_slots = 2 * sp.side_parts;
-  sp.shared_slots = 2 * sp.shared_parts;
+  // Items: fewer than one more than steps / step for every tile, which is up to twice the parts wanted.
+  const int64_t tiles = all_rows / kRowTile + seqs;
+  sp.side_items = seqs + sp.side_parts;
+  sp.shared_items = shared ? tiles + 2 * sp.shared_parts : 0;
+  // Those of tiles in several parts: ceil(x) < 2 x for x > 1.
+  sp.side_slots = (int)std::min<int64_t>(2 * sp.side_parts, seqs * kMostParts);
+  sp.shared_slots = (int)std::min<int64_t>(4 * sp.shared_parts, tiles * kMostParts);
   sp.side_floats = (size_t)sp.side_slots * n_kv_heads * kPartFloats;
   sp.shared_floats = (size_t)sp.shared_slots * n_kv_heads * 4 * kPartFloats;
   return sp;
@@ -663,17 +826,28 @@ PromptSplit prompt_split(int batch, int n_kv_heads, int n_rep, int n_tokens, int
 
 // FIER_ESHAPE where the grid would not fit 32 bits, else FIER_OK or FIER_EHIP.
 int launch_prompt_attn(int dtype, PromptArgs a, const PromptSplit& sp, hipStream_t st) {
-  const int64_t grid = sp.side_grid + sp.shared_grid;
+  const int64_t items = sp.side_items + sp.shared_items;
   if (a.max_new == 0) return FIER_OK;
-  if (grid > INT32_MAX) return FIER_ESHAPE;
-  a.side_grid = (int)sp.side_grid;
+  if (items * a.n_kv_heads > INT32_MAX) return FIER_ESHAPE;
+  a.side_items = (int)sp.side_items;
   a.side_parts = sp.side_parts, a.shared_parts = sp.shared_parts;
   a.side_slots = sp.side_slots, a.shared_slots = sp.shared_slots;
   a.shared_partials = a.side_partials + sp.side_floats;
-  if (dtype == DT_F16)
-    prompt_attn_kernel<DT_F16><<<(unsigned)grid, 256, 0, st>>>(a);
-  else
-    prompt_attn_kernel<DT_BF16><<<(unsigned)grid, 256, 0, st>>>(a);
+  auto over = [&](int64_t n) {
+    return dim3((unsigned)a.n_kv_heads, (unsigned)std::min<int64_t>(n, kGridY), (unsigned)((n + kGridY - 1) / kGridY));
+  };
+  const dim3 grid = over(items), join = over(sp.shared_items);
+  const bool cache = a.seq_lens != nullptr;
+#define FIER_PROMPT(DT)                                              \
+  if (cache) prompt_attn_kernel<DT, true><<<grid, 256, 0, st>>>(a);  \
+  else prompt_attn_kernel<DT, false><<<grid, 256, 0, st>>>(a);       \
+  if (sp.shared_parts) prompt_join_kernel<DT><<<join, 256, 0, st>>>(a)
+  if (dtype == DT_F16) {
+    FIER_PROMPT(DT_F16);
+  } else {
+    FIER_PROMPT(DT_BF16);
+  }
+#undef FIER_PROMPT
   return hipGetLastError() == hipSuccess ? FIER_OK : FIER_EHIP;
 }
 

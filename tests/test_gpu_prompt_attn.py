@@ -208,6 +208,54 @@ def test_long_chunks_behind_long_contexts(dtype, n_q, n_kv, first, new):
     check_chunk(run_chunk(cfg, cache, q, [new]), q, rows, [first], [new], cfg)
 
 
+def test_many_tiles_and_parts_of_unequal_numbers():
+    """One call with every way a tile's rows are split: 48 parts in groups and fewer, single tokens beside them; then far more tiles
+    than there are counters for groups.  The workspace is left ready each time."""
+    cfg = B.make_config(5, 8, 1, 16384, BF16)
+    first, new = [9000, 16000, 3000, 0, 12000], [150, 4, 17, 900, 1]
+    rows, cache = make_cache(cfg, first, new, BF16, 64, 80)
+    q = randn((sum(new), 8, D), BF16, 81)
+    ws = B.make_chunk_workspace(cfg, sum(new), max(new))
+    for _ in range(2):
+        check_chunk(run_chunk(cfg, cache, q, new, ws=ws), q, rows, first, new, cfg)
+    for n, lo in ((1010, 2000), (8200, 300)):
+        cfg = B.make_config(1, 8, 1, 16384, BF16)
+        rows, cache = make_cache(cfg, [lo], [n], BF16, 64, 82)
+        q = randn((n, 8, D), BF16, 83)
+        ws = B.make_chunk_workspace(cfg, n, n)
+        out = [run_chunk(cfg, cache, q, [n], ws=ws) for _ in range(2)]
+        assert torch.equal(*out)
+        k, v = (t[0].transpose(0, 1) for t in rows)
+        for at in sorted({0, 1, 500, n - 700, n - 1}):  # single rows of it
+            want, tol = attention64(q[at:at + 1], k, v, lo + at, cfg.sm_scale)
+            check_attention(out[0][at:at + 1], want, tol, str(at))
+
+
+def test_a_batch_of_more_sequences_than_lanes():
+    """130 sequences, tokens in every third."""
+    n = 130
+    cfg = B.make_config(n, 4, 2, 640, F16)
+    rng = np.random.default_rng(3)
+    first = rng.integers(0, 500, n).tolist()
+    new = [int(rng.integers(1, 100)) if b % 3 == 0 else (b % 2 if b > 100 else 0) for b in range(n)]
+    rows, cache = make_cache(cfg, first, new, F16, 0, 84)
+    q = randn((sum(new), 4, D), F16, 85)
+    check_chunk(run_chunk(cfg, cache, q, new, pad=2), q, rows, first, new, cfg)
+
+
+def test_offsets_that_make_no_sense_leave_the_workspace_ready():
+    """Sequences that share tokens, more of them than there are tokens: whatever comes out, the next call is right."""
+    cfg = B.make_config(6, 2, 1, 4096, BF16)
+    first, new = [4000, 3000, 2000, 4000, 10, 500], [10, 0, 40, 1, 30, 2]
+    rows, cache = make_cache(cfg, first, new, BF16, 0, 86)
+    q = randn((sum(new), 2, D), BF16, 87)
+    ws = B.make_chunk_workspace(cfg, sum(new), max(new))
+    out = torch.zeros(sum(new), 2, D, dtype=torch.bfloat16, device="cuda")
+    for bad in ([0, 83, 0, 83, 0, 83, 0], [83, 0, 1 << 30, -1, 50, 20, 83], [-5, 40, 0, 40, 0, 40, 83]):
+        B.chunk_attn(cfg, cache, q.cuda(), i32(bad), 83, out, ws)
+    check_chunk(run_chunk(cfg, cache, q, new, ws=ws), q, rows, first, new, cfg)
+
+
 def test_a_full_cache():
     """Tokens past the capacity attend over all of its rows; lengths above it count as full, below 0 as empty."""
     cfg = B.make_config(3, 4, 2, 256, BF16)
