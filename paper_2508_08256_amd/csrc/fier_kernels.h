@@ -233,7 +233,7 @@ struct PromptArgs {  // attention of the new tokens (passed to the kernel by val
   int n_tokens, max_new, kv_cap;  // kv_cap: rows of a cache; no limit without one
   float *side_partials, *shared_partials;
   uint32_t* counters;  // kSelBins words per unit, zero between calls
-  int side_items, side_parts, shared_parts, side_slots, shared_slots;  // from PromptSplit
+  int side_items, parts_wanted, side_slots, shared_slots;  // from PromptSplit
   uint32_t per_rep;  // ceil(2^31 / n_rep)
   // row / n_rep for rows below 2^27: the quotient's error, row * (per_rep n_rep - 2^31) < 2^27 * 8, stays below 2^31
   __device__ __forceinline__ int token_of(int row) const { return (int)__umulhi(2u * (uint32_t)row, per_rep); }
@@ -251,7 +251,7 @@ struct PromptArgs {  // attention of the new tokens (passed to the kernel by val
 };
 struct PromptSplit {  // how the launch is cut
   int64_t side_items, shared_items;   // workgroups per kv head
-  int side_parts, shared_parts;       // parts of K / V rows wanted per kv head; 0: nothing is split
+  int parts;                          // of K / V rows wanted per kv head; 0: nothing is split
   int side_slots, shared_slots;       // partial results per kv head
   size_t side_floats, shared_floats;  // of all of them
 };

@@ -223,33 +223,27 @@ struct Rows32 {
     large = false;
   }
 
-  // at: bytes from the tiles that `r` was made for
-  template <int M>
-  __device__ __forceinline__ static void scores(const LdsReads& r, int at, const uint4 (&q)[8], floatx16_t (&s)[M]) {
+  // Logits of 32 tokens.  at: bytes from the tiles that `r` was made for.
+  __device__ __forceinline__ static floatx16_t scores(const LdsReads& r, int at, const uint4 (&q)[8]) {
+    floatx16_t s = {0.f};
 #pragma unroll
-    for (int mt = 0; mt < M; ++mt) {
-      s[mt] = floatx16_t{0.f};
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s[mt] = mfma_32x32x16<DT>(lds_read16(r.k[k] + (at + mt * 32 * kRowBytes)), q[k], s[mt]);
-    }
+    for (int k = 0; k < 8; ++k) s = mfma_32x32x16<DT>(lds_read16(r.k[k] + at), q[k], s);
+    return s;
   }
 
-  // Logits into weights, the running maximum and sum with them.  left: how many of the tile's tokens the row attends over
-  // (only looked at if masked).
-  template <int M>
-  __device__ __forceinline__ void weights(floatx16_t (&s)[M], float c, bool masked, int left, int h) {
+  // Logits into weights, the running maximum and sum with them.  left: how many of the tokens the row attends over (only
+  // looked at if masked).
+  __device__ __forceinline__ void weights(floatx16_t& s, float c, bool masked, int left, int h) {
     if (masked) {
 #pragma unroll
-      for (int mt = 0; mt < M; ++mt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[mt][i] = mt * 32 + 8 * (i >> 2) + (i & 3) < left - 4 * h ? s[mt][i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < left - 4 * h ? s[i] : -INFINITY;
     }
-    float mx = s[0][0];
+    float mx = s[0];
 #pragma unroll
-    for (int i = 1; i < 16 * M; ++i) mx = larger(mx, s[i >> 4][i & 15]);
+    for (int i = 1; i < 16; ++i) mx = larger(mx, s[i]);
     mx = halves_max(mx);
     const float top = rounded_product(mx, c) - kBias;
-    if (__any(top > (large ? m : m + kSlack))) {
+    if (__any(top > (large ? m : m + kSlack))) {  // the maxima settle after a few tiles
       const float to = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - to);
       m = to;
       l *= alpha;
@@ -261,23 +255,22 @@ struct Rows32 {
     // distance from the rounded maximum would be that one's rounding error: there both are rounded alike.
     if (__builtin_expect(large, 0)) {
 #pragma unroll
-      for (int i = 0; i < 16 * M; ++i) s[i >> 4][i & 15] = __builtin_amdgcn_exp2f(rounded_product(s[i >> 4][i & 15], c) - m);
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(rounded_product(s[i], c) - m);
     } else {
 #pragma unroll
-      for (int i = 0; i < 16 * M; ++i) s[i >> 4][i & 15] = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], c, -m));
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -m));
     }
 #pragma unroll
-    for (int i = 0; i < 16 * M; ++i) l += s[i >> 4][i & 15];
+    for (int i = 0; i < 16; ++i) l += s[i];
   }
 
-  template <int M>
-  __device__ __forceinline__ void add_values(const LdsReads& r, int at, const floatx16_t (&p)[M]) {
+  // The weights, rounded to the K dtype (to nearest: with bf16 by 2^-9 of each at most, about as much again in the sum of many as
+  // the rounding of the output; three exact parts as in the decode step would make it three products), times V.
+  __device__ __forceinline__ void add_values(const LdsReads& r, int at, const floatx16_t& p) {
 #pragma unroll
-    for (int t = 0; t < 2 * M; ++t) {
-      const int i = 8 * (t & 1);
-      const floatx16_t& x = p[t >> 1];
-      const uint4 pb = make_uint4(pack2<DT>(x[i], x[i + 1]), pack2<DT>(x[i + 2], x[i + 3]), pack2<DT>(x[i + 4], x[i + 5]),
-                                  pack2<DT>(x[i + 6], x[i + 7]));
+    for (int t = 0; t < 2; ++t) {
+      const uint4 pb = make_uint4(pack2<DT>(p[8 * t], p[8 * t + 1]), pack2<DT>(p[8 * t + 2], p[8 * t + 3]),
+                                  pack2<DT>(p[8 * t + 4], p[8 * t + 5]), pack2<DT>(p[8 * t + 6], p[8 * t + 7]));
 #pragma unroll
       for (int ct = 0; ct < 4; ++ct) {
         const lds_char* const from = r.v[ct] + (at + t * 16 * kRowBytes);
@@ -312,88 +305,76 @@ struct QueryRow {
   }
 };
 
-// ---- partial results of a part of the K / V rows ------------------------------------------------------------------------------
-// Per 32 query rows: o as the lanes hold it (four channel tiles of 16 floats a lane), then m and l of every lane.  Written through
-// to memory and read past the caches: another workgroup of the launch reads them (see arrive_add).  Only lanes whose row is
-// there take part.
+// ---- partial results of side-by-side parts ---------------------------------------------------------------------------------
+// o of 32 query rows as the lanes hold it (four channel tiles of 16 floats a lane), then m and l of every lane.  Written through to
+// memory and read past the caches: another workgroup of the launch reads them (see arrive_add).  Only lanes whose row is there
+// take part: with one token of four heads an eighth of them.
 constexpr int kPartFloats = 32 * kD + 2 * 64;
-__device__ __forceinline__ void store_partial(float* slot, int ct, const floatx16_t& o, int lane) {
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+  return (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32;
+}
+__device__ __forceinline__ float low_of(unsigned long long w) { return __uint_as_float((uint32_t)w); }
+__device__ __forceinline__ float high_of(unsigned long long w) { return __uint_as_float((uint32_t)(w >> 32)); }
+__device__ __forceinline__ void store_partial(float* slot, int ct, const floatx16_t& o, float m, float l, int lane) {
   unsigned long long* const p = reinterpret_cast<unsigned long long*>(slot + ct * 1024) + lane;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    store_coherent(p + i * 64, (unsigned long long)__float_as_uint(o[2 * i]) | (unsigned long long)__float_as_uint(o[2 * i + 1]) << 32);
+  for (int i = 0; i < 8; ++i) store_coherent(p + i * 64, pair_of(o[2 * i], o[2 * i + 1]));
+  if (ct == 0) store_coherent(reinterpret_cast<unsigned long long*>(slot + 32 * kD) + lane, pair_of(m, l));
 }
-__device__ __forceinline__ void store_partial_sums(float* slot, float m, float l, int lane) {
-  store_coherent(reinterpret_cast<unsigned long long*>(slot + 32 * kD) + lane,
-                 (unsigned long long)__float_as_uint(m) | (unsigned long long)__float_as_uint(l) << 32);
-}
-// Channel tiles ct0 .. ct0 + CT - 1 of n slots, `pitch` floats apart, joined; BATCH slots' loads are under way together.
-template <int CT, int BATCH>
-__device__ __forceinline__ void join_partials(const float* slots, size_t pitch, int n, int ct0, int lane, floatx16_t (&o)[CT],
-                                              float& m, float& l) {
+// Channel tile ct of n slots, `pitch` floats apart, joined, the loads of eight under way together.
+__device__ __forceinline__ void join_partials(const float* slots, size_t pitch, int n, int ct, int lane, floatx16_t& o, float& m,
+                                              float& l) {
+  constexpr int kBatch = 8;
   m = -FLT_MAX, l = 0.f;
+  o = floatx16_t{0.f};
+  for (int p0 = 0; p0 < n; p0 += kBatch) {
+    unsigned long long ml[kBatch], w[kBatch][8];
 #pragma unroll
-  for (int c = 0; c < CT; ++c) o[c] = floatx16_t{0.f};
-  for (int p0 = 0; p0 < n; p0 += BATCH) {
-    unsigned long long ml[BATCH], w[BATCH][CT][8];
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) {
+    for (int k = 0; k < kBatch; ++k) {
       const float* const slot = slots + (size_t)min(p0 + k, n - 1) * pitch;
       ml[k] = load_coherent(reinterpret_cast<const unsigned long long*>(slot + 32 * kD) + lane);
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          w[k][c][i] = load_coherent(reinterpret_cast<const unsigned long long*>(slot + (ct0 + c) * 1024) + i * 64 + lane);
+      for (int i = 0; i < 8; ++i) w[k][i] = load_coherent(reinterpret_cast<const unsigned long long*>(slot + ct * 1024) + i * 64 + lane);
     }
     float to = m;
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k) to = fmaxf(to, __uint_as_float((uint32_t)ml[k]));
+    for (int k = 0; k < kBatch; ++k) to = fmaxf(to, low_of(ml[k]));
     const float alpha = __builtin_amdgcn_exp2f(m - to);
     m = to;
     l *= alpha;
+    o *= alpha;
 #pragma unroll
-    for (int c = 0; c < CT; ++c) o[c] *= alpha;
+    for (int k = 0; k < kBatch; ++k) {
+      const float f = p0 + k < n ? __builtin_amdgcn_exp2f(low_of(ml[k]) - m) : 0.f;
+      l += f * high_of(ml[k]);
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k) {
-      const float f = p0 + k < n ? __builtin_amdgcn_exp2f(__uint_as_float((uint32_t)ml[k]) - m) : 0.f;
-      l += f * __uint_as_float((uint32_t)(ml[k] >> 32));
-#pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          o[c][2 * i] += f * __uint_as_float((uint32_t)w[k][c][i]);
-          o[c][2 * i + 1] += f * __uint_as_float((uint32_t)(w[k][c][i] >> 32));
-        }
+      for (int i = 0; i < 8; ++i) o[2 * i] += f * low_of(w[k][i]), o[2 * i + 1] += f * high_of(w[k][i]);
     }
   }
 }
 
-constexpr int kSideTile = 32;    // rows of K and V per wavefront and step where the wavefronts go side by side
-constexpr int kSideWaves = 3;    // of four: three such workgroups fit a CU's LDS
-constexpr int kSideStep = kSideWaves * kSideTile;
-#ifndef SIDEL
-#define SIDEL 2
-#endif
-#ifndef SHAREDL
-#define SHAREDL 8
-#endif
-constexpr int kSideLeast = SIDEL;    // steps of a part there, at least
-constexpr int kSharedLeast = SHAREDL;  // steps of 64 rows of a part where the wavefronts share the tiles, at least
-// Parts of a tile: up to 8 are joined by the last of its workgroups; more by the last of every group of 7 or fewer, and the groups
-// by the last of them (one workgroup reads 3 MB of 48 parts of 128 rows in 25 us, meanwhile nobody else has work).  A tile's
-// counters: one for the whole and one for each group; a sequence of more tiles than there is room for has up to 8 parts, and
-// one of more still is not split.
-constexpr int kGroup = 8, kMostParts = 48;
-constexpr float kStreamBytes = 64 << 20;  // K and V rows from here on take the streaming hint (side by side)
-constexpr unsigned kGridY = 32768;  // items along y, the rest along z
-
 // ---- which workgroup does what -----------------------------------------------------------------------------------------------
 // A sequence's query rows per kv head are cut into tiles of 128; the last one, where it has at most 32, goes through its K / V
-// rows side by side, the others share them.  Where there are partial results to hand on (a cache's workspace), the K / V rows of
-// a tile are split into parts of `step` steps, one length for all sequences of the call, so that unequal ones keep the GPU busy to
-// the end: `step` is the call's steps over the number of parts wanted.  Lengths lie on the GPU, so every workgroup works
-// this out for itself, one sequence a lane.
+// rows side by side, the others share them.  Over a cache the K / V rows of a tile are split into parts of `step` steps, one length
+// for all sequences of the call, so that unequal ones keep the GPU busy to the end: `step` is the call's steps over the
+// number of parts wanted, about as many as the GPU holds workgroups of this kernel at once (256 CUs x 3).  Lengths lie on the GPU,
+// so every workgroup works this out for itself, one sequence a lane.  us with one number of parts for all sequences / this: chunks
+// of 1 to 500 tokens of 8 sequences of up to 12000, 24 q / 8 kv heads 458 / 270; one token of 16 sequences of 8k-64k 531 / 485.
+constexpr int kSideTile = 32;    // rows of K and V per wavefront and step side by side
+constexpr int kSideWaves = 3;    // of the four: so three such workgroups fit a CU's LDS
+constexpr int kSideStep = kSideWaves * kSideTile;
+constexpr int kSideLeast = 2;    // steps of a part, at least
+constexpr int kSharedLeast = 8;  // steps of 64 rows of a part of shared rows, at least
+// Parts of a tile, at most.  Side by side, up to 8 are joined by the last of their workgroups; more in groups of up to 7 by the last of
+// each, and the groups by the last of those: eight counters.  Up to 64 steps are not worth the second round: 2 x 2000 tokens, 8 kv heads
+// 16.0 us in 11 parts, 12.0 in 8.
+constexpr int kGroup = 8, kMostParts = 48;
+constexpr int kPartsWanted = 768;
+// From so many bytes of K and V on, side-by-side tiles are loaded with the streaming hint, as the other gathers do it: one token of 16
+// sequences of 8k-64k 528 / 484 us (2.8 GB, 5.9 TB/s), of 128k 114 / 104; 134 MB, which the last cache can hold, 42 / 46.
+constexpr float kStreamBytes = 64 << 20;
+constexpr unsigned kGridY = 32768;  // items along y, the rest along z
+
 struct SequenceWork {
   PromptSpan sp;
   int n_rows, tiles, aside;  // tiles of shared rows; rows of the side-by-side tile or 0
@@ -418,7 +399,7 @@ struct SequenceWork {
     return SIDE ? (n_kv + kSideStep - 1) / kSideStep : (n_kv + kTile - 1) / kTile;
   }
   template <bool SIDE>
-  __device__ __forceinline__ int parts(int step) const {  // that its tiles have at most; more tiles than counters: not split
+  __device__ __forceinline__ int parts(int step) const {  // that its last tile has
     const int n = steps<SIDE>();
     return n <= step ? 1 : min((n + step - 1) / step, SIDE && n <= kGroup * kGroup ? kGroup : kMostParts);
   }
@@ -458,9 +439,11 @@ __device__ __forceinline__ bool find_item(const PromptArgs& a, int j, int lane, 
     count(w0);
     int64_t tokens = tokens0;
     for (int b0 = 64; b0 < a.batch; b0 += 64) count(SequenceWork(a, b0 + lane, lane, tokens));
-    // A tile of s steps becomes ceil(s / step) items, half of one more than s / step on average.
-    const float parts = (float)(SIDE ? a.side_parts : a.shared_parts);
-    const float wanted = SIDE || tiles > 1.2f * parts ? (SIDE ? 1.f : 2.f) * parts : (tiles > 0.6f * parts ? 2.f : 1.f) * parts - 0.5f * tiles;
+    // A tile of s steps becomes ceil(s / step) items, half of one more than s / step on average.  Shared tiles take the GPU for
+    // long: their items are to fit one round, two where the tiles alone nearly fill one; many tiles are split where one has
+    // more than its share of two rounds.
+    float wanted = (float)a.parts_wanted;
+    if (!SIDE) wanted = tiles > 1.2f * wanted ? 2.f * wanted : (tiles > 0.6f * wanted ? 2.f : 1.f) * wanted - 0.5f * tiles;
     it.step = __builtin_amdgcn_readfirstlane(max(SIDE ? kSideLeast : kSharedLeast, (int)ceilf(all / wanted)));
     it.stream = all * (float)a.n_kv_heads * (2.f * kSideStep * kRowBytes) >= kStreamBytes;
   }
@@ -490,20 +473,12 @@ __device__ __forceinline__ bool find_item(const PromptArgs& a, int j, int lane, 
   return false;
 }
 
-// One part of n_parts is done: its partial results (channel tiles ct0 .. ct0 + CT - 1 of the wavefront's lanes that are there) go
-// to its slot, and the last workgroup of all returns true with those of all parts joined in o, m and l.
-template <int CT, int BATCH>
-__device__ __forceinline__ bool join_parts(float* slots, size_t pitch, int n_parts, int part, uint32_t* counters, bool there, int ct0,
-                                           bool sums, int wave, int lane, floatx16_t (&o)[CT], float& m, float& l, uint32_t* flag) {
+// Part `part` of n_parts is done: its partial results (channel tile `wave` of the lanes that are there) go to its slot, and the last
+// workgroup of all returns true with those of all parts joined in o, m and l.
+__device__ __forceinline__ bool join_parts(float* slots, int n_parts, int part, uint32_t* counters, bool there, int wave, int lane,
+                                           floatx16_t& o, float& m, float& l, uint32_t* flag) {
   const bool first = wave == 0 && lane == 0;
-  auto put = [&](int at) {
-    if (!there) return;
-    float* const slot = slots + (size_t)at * pitch;
-#pragma unroll
-    for (int c = 0; c < CT; ++c) store_partial(slot, ct0 + c, o[c], lane);
-    if (sums) store_partial_sums(slot, m, l, lane);
-  };
-  put(part);
+  if (there) store_partial(slots + (size_t)part * kPartFloats, wave, o, m, l, lane);
   int group = 1, n = n_parts;  // parts per group, groups
   if (n_parts > kGroup) {
     group = 3;
@@ -511,12 +486,15 @@ __device__ __forceinline__ bool join_parts(float* slots, size_t pitch, int n_par
     n = (n_parts + group - 1) / group;
     const int g = part / group, size = min(group, n_parts - g * group);
     if (arrive_add(counters + 1 + g, 1u, flag, first) != (uint32_t)size - 1) return false;
-    if (there) join_partials<CT, BATCH>(slots + (size_t)(g * group) * pitch, pitch, size, ct0, lane, o, m, l);
+    float* const mine = slots + (size_t)(g * group) * kPartFloats;  // the group's first slot takes the group's results
+    if (there) join_partials(mine, kPartFloats, size, wave, lane, o, m, l);
+    wait_loads<0>();
+    meet();  // every wavefront has read the sums there
+    if (there) store_partial(mine, wave, o, m, l, lane);
     if (first) store_coherent(counters + 1 + g, 0u);
-    put(g * group);
   }
   if (arrive_add(counters, 1u, flag, first) != (uint32_t)n - 1) return false;
-  if (there) join_partials<CT, BATCH>(slots, pitch * group, n, ct0, lane, o, m, l);
+  if (there) join_partials(slots, (size_t)group * kPartFloats, n, wave, lane, o, m, l);
   if (first) store_coherent(counters, 0u);
   return true;
 }
@@ -526,7 +504,7 @@ template <int DT, bool CACHE>
 __device__ __forceinline__ void join_side_by_side(const PromptArgs& a, const Item& it, int head, const Rows32<DT>& st, int wave,
                                                   lds_char* lds, uint32_t* flag) {
   const int lane = lane_again(), h = lane >> 5;
-  const int unit = it.b * a.n_kv_heads + head, n_rows = it.sp.n * a.n_rep, part = it.at, n_parts = it.parts;
+  const int unit = it.b * a.n_kv_heads + head, n_rows = it.sp.n * a.n_rep;
   const QueryRow row(a, it.sp, head, n_rows / kRowTile * kRowTile + (lane & 31), n_rows);
   const float l = halves_sum(st.l);
   typedef __attribute__((address_space(3))) float lds_float;
@@ -549,25 +527,25 @@ __device__ __forceinline__ void join_side_by_side(const PromptArgs& a, const Ite
     of[w] = ml[w * 64 + lane];
     m = fmaxf(m, of[w].x);
   }
-  floatx16_t o[1] = {floatx16_t{0.f}};
+  floatx16_t o = {0.f};
 #pragma unroll
   for (int w = 0; w < kSideWaves; ++w) {
     const float f = __builtin_amdgcn_exp2f(of[w].x - m);
     sum += f * of[w].y;
     const lds_float* const p = (const lds_float*)(lds + w * 2 * kSideTile * kRowBytes);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[0][i] += f * p[(wave * 16 + i) * 64 + lane];
+    for (int i = 0; i < 16; ++i) o[i] += f * p[(wave * 16 + i) * 64 + lane];
   }
-  if (CACHE && n_parts > 1 && !join_parts<1, 8>(a.side_partials + ((size_t)head * a.side_slots + it.slot) * kPartFloats, kPartFloats, n_parts,
-                                       part, a.counters + (size_t)unit * kSelBins, row.there, wave, wave == 0, wave, lane, o, m,
-                                       sum, flag))
+  if (CACHE && it.parts > 1 &&
+      !join_parts(a.side_partials + ((size_t)head * a.side_slots + it.slot) * kPartFloats, it.parts, it.at,
+                  a.counters + (size_t)unit * kSelBins, row.there, wave, lane, o, m, sum, flag))
     return;
-  if (row.there) store_channels<DT>(row.out, wave, h, o[0], sum > 0.f ? 1.f / sum : 0.f);
+  if (row.there) store_channels<DT>(row.out, wave, h, o, sum > 0.f ? 1.f / sum : 0.f);
 }
 
-// Up to 32 query rows: all four wavefronts hold them and go side by side through the K / V rows, each through 32 of every 128,
-// in 16 KiB of LDS of its own, so that nobody waits for anybody.  The next K rows are loaded once this step's logits are
-// there, the next V rows after its product.  Bound by memory.
+// Up to 32 query rows: three wavefronts hold them all and go side by side through the K / V rows, each through 32 of every 96, in
+// 16 KiB of LDS of its own, so that nobody waits for anybody.  The next K rows are loaded once this step's logits are there, the
+// next V rows after its product.  Bound by memory: nine wavefronts with 8 to 16 KiB under way each on a CU.
 template <int DT, bool CACHE>
 __device__ __forceinline__ void attend_side_by_side(const PromptArgs& a, const Item& it, int head, lds_char* lds, uint32_t* flag) {
   const PromptSpan sp = it.sp;
@@ -602,9 +580,8 @@ __device__ __forceinline__ void attend_side_by_side(const PromptArgs& a, const I
   for (; t0 < stop; t0 += kSideStep) {
     const int next = t0 + kSideStep < stop ? t0 + kSideStep : t0;  // the last step loads its own rows once more
     const size_t r = rows.row(block, next);
-    floatx16_t s[1];
     wait_loads<8>();
-    Rows32<DT>::scores(reads, 0, q, s);
+    floatx16_t s = Rows32<DT>::scores(reads, 0, q);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, kt, 0, it.stream);
     block = rows.block_of(next + kSideStep < stop ? next + kSideStep : next);  // for the step after the next: the list is far away
@@ -617,6 +594,7 @@ __device__ __forceinline__ void attend_side_by_side(const PromptArgs& a, const I
   wait_loads<0>();
   join_side_by_side<DT, CACHE>(a, it, head, st, wave, lds, flag);
 }
+
 // Which tile and part of a sequence's shared rows an item is; the tiles that attend over the most rows come first.
 struct SharedTile {
   int tiles, turned, tile, part, n_kv, all, n_parts;  // n_kv rows, `all` steps; a prompt's first tiles have fewer than the last
@@ -633,6 +611,8 @@ struct SharedTile {
 };
 
 // ---- shared tiles in several parts: a second launch joins them ------------------------------------------------------------------
+// Joined by the last workgroup of each tile, as the side-by-side ones are, it was one CU that read up to 3 MB: 64 tokens of 32 q / 8 kv
+// heads behind 32768 took 93 us, now 62.
 // Per wavefront o as the lanes hold it, 16 chunks of 64 x 4 floats (channel tile ct, channels 8 i + 4 h + 0..3: chunk 4 ct + i),
 // then m and l of the lanes.
 __device__ __forceinline__ float* shared_slot(const PromptArgs& a, const Item& it, int head, int turned, int part) {
@@ -720,7 +700,14 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
   else join_chunks<DT, 1, 16>(a, it, head, t, first, lane);
 }
 
-// 128 query rows, 32 a wavefront; the K / V rows go through LDS 64 at a time, two tiles of each, shared by the wavefronts.
+// 128 query rows, 32 a wavefront; the K / V rows go through LDS 64 at a time, shared by the wavefronts: two tiles of K, whose next
+// one is loaded a step ahead, and one of V, loaded during the step's first logits.  48 KiB and at most 168 registers, so that
+// three workgroups share a CU and one's products run beside another's exponentials.
+//   What bounds it: power.  At 16384 tokens of 32 heads (2.09 ms, 1.05 PFLOP/s; a large library product of random numbers makes
+// 1.2) the matrix cores are busy 56 % of the cycles, at 1.6 GHz.  Two workgroups per CU with twice the registers, each
+// wavefront's exponentials interleaved with its next products, were busy 50 % at 1.74 GHz: 2.30 ms.  64 rows a wavefront
+// (half the LDS reads) needs accumulation registers and the moves to and from them: 2.83.  Fewer instructions pay: addresses in
+// registers instead of made anew 2.16 -> 2.09.
 template <int DT, bool CACHE>
 __device__ __forceinline__ void attend_shared(const PromptArgs& a, const Item& it, int head, lds_char* lds) {
   const PromptSpan sp = it.sp;
@@ -758,16 +745,16 @@ __device__ __forceinline__ void attend_shared(const PromptArgs& a, const Item& i
     r = rows.row(block, next);
     kl.load(rows.k + r * rows.k_stride, rows.k_stride, n_kv - next, lds + (cur ^ 1) * kBytes, wave);
     block = rows.block_of(min(i + 2, end - 1) * kTile);
-    floatx16_t s[1];
+    floatx16_t s;
     if (t0 < most) {  // some of the wavefront's rows go that far
-      Rows32<DT>::scores(reads, cur * kBytes, q, s);
+      s = Rows32<DT>::scores(reads, cur * kBytes, q);
       st.weights(s, a.scale, t0 + 32 > least, row.lim - t0, h);
     }
     wait_loads<4>();
     meet();
     if (t0 < most) st.add_values(reads, 0, s);
     if (t0 + 32 < most) {
-      Rows32<DT>::scores(reads, cur * kBytes + 32 * kRowBytes, q, s);
+      s = Rows32<DT>::scores(reads, cur * kBytes + 32 * kRowBytes, q);
       st.weights(s, a.scale, t0 + kTile > least, row.lim - t0 - 32, h);
       st.add_values(reads, 32 * kRowBytes, s);
     }
@@ -781,8 +768,7 @@ __device__ __forceinline__ void attend_shared(const PromptArgs& a, const Item& i
 }
 
 // The grid lists the side-by-side items first, then the shared ones, the kv heads of an item next to each other: with a multiple
-// of 8 of them a head's K and V stay in one XCD's L2.  What has no work leaves at once.  A tile whose K / V rows are split hands
-// its partial results to the last of its workgroups.
+// of 8 of them a head's K and V stay in one XCD's L2.  What has no work leaves at once.
 //   CACHE: over a cache's rows, split where there are few tiles; else packed prompts, not split.
 template <int DT, bool CACHE>
 __global__ __launch_bounds__(256, 3) void prompt_attn_kernel(PromptArgs a) {
@@ -798,27 +784,19 @@ __global__ __launch_bounds__(256, 3) void prompt_attn_kernel(PromptArgs a) {
   }
 }
 
-#ifndef SIDE_T
-#define SIDE_T 768
-#endif
-#ifndef SHARED_T
-#define SHARED_T 768
-#endif
 // How the launch is cut.
 PromptSplit prompt_split(int batch, int n_kv_heads, int n_rep, int n_tokens, int max_new, bool split) {
   PromptSplit sp = {};
   const int64_t rows = (int64_t)max_new * n_rep, all_rows = (int64_t)n_tokens * n_rep;
+  const int64_t seqs = std::min(batch, n_tokens), tiles = all_rows / kRowTile + seqs;
   const bool shared = rows > kSideRows;  // some sequence may have more rows than go side by side
-  const int64_t seqs = std::min(batch, n_tokens);
-  sp.side_parts = split ? std::max(1, SIDE_T / n_kv_heads) : 0;
-  sp.shared_parts = split && shared ? std::max(1, SHARED_T / n_kv_heads) : 0;
-  // Items: fewer than one more than steps / step for every tile, which is up to twice the parts wanted.
-  const int64_t tiles = all_rows / kRowTile + seqs;
-  sp.side_items = seqs + sp.side_parts;
-  sp.shared_items = shared ? tiles + 2 * sp.shared_parts : 0;
+  sp.parts = split ? std::max(1, kPartsWanted / n_kv_heads) : 0;
+  // Items: fewer than steps / step + 1 of every tile; shared tiles want up to twice the parts.
+  sp.side_items = seqs + sp.parts;
+  sp.shared_items = shared ? tiles + 2 * sp.parts : 0;
   // Those of tiles in several parts: ceil(x) < 2 x for x > 1.
-  sp.side_slots = (int)std::min<int64_t>(2 * sp.side_parts, seqs * kMostParts);
-  sp.shared_slots = (int)std::min<int64_t>(4 * sp.shared_parts, tiles * kMostParts);
+  sp.side_slots = (int)std::min<int64_t>(2 * sp.parts, seqs * kMostParts);
+  sp.shared_slots = shared ? (int)std::min<int64_t>(4 * sp.parts, tiles * kMostParts) : 0;
   sp.side_floats = (size_t)sp.side_slots * n_kv_heads * kPartFloats;
   sp.shared_floats = (size_t)sp.shared_slots * n_kv_heads * 4 * kPartFloats;
   return sp;
@@ -830,7 +808,7 @@ int launch_prompt_attn(int dtype, PromptArgs a, const PromptSplit& sp, hipStream
   if (a.max_new == 0) return FIER_OK;
   if (items * a.n_kv_heads > INT32_MAX) return FIER_ESHAPE;
   a.side_items = (int)sp.side_items;
-  a.side_parts = sp.side_parts, a.shared_parts = sp.shared_parts;
+  a.parts_wanted = sp.parts;
   a.side_slots = sp.side_slots, a.shared_slots = sp.shared_slots;
   a.shared_partials = a.side_partials + sp.side_floats;
   auto over = [&](int64_t n) {
@@ -841,7 +819,7 @@ int launch_prompt_attn(int dtype, PromptArgs a, const PromptSplit& sp, hipStream
 #define FIER_PROMPT(DT)                                              \
   if (cache) prompt_attn_kernel<DT, true><<<grid, 256, 0, st>>>(a);  \
   else prompt_attn_kernel<DT, false><<<grid, 256, 0, st>>>(a);       \
-  if (sp.shared_parts) prompt_join_kernel<DT><<<join, 256, 0, st>>>(a)
+  if (sp.shared_slots) prompt_join_kernel<DT><<<join, 256, 0, st>>>(a)
   if (dtype == DT_F16) {
     FIER_PROMPT(DT_F16);
   } else {
