@@ -1,5 +1,6 @@
 """Causal attention of prompts and of chunks of new tokens over a cache, against the formula in 64 bits."""
 import math
+import os
 
 import numpy as np
 import pytest
@@ -306,3 +307,143 @@ def test_results_do_not_change_from_call_to_call():
     ref = run_chunk(cfg, cache, q, [3, 1], ws=ws)
     for _ in range(10):
         assert torch.equal(run_chunk(cfg, cache, q, [3, 1], ws=ws), ref)
+
+
+def test_only_padding():
+    """Rows in the arrays, no tokens in any sequence."""
+    cfg = B.make_config(3, 4, 2, 256, BF16)
+    rows, cache = make_cache(cfg, [0, 5, 256], [0, 0, 0], BF16, 0, 90)
+    q = torch.zeros(0, 4, D, dtype=torch.bfloat16)
+    assert bool((run_chunk(cfg, cache, q, [0, 0, 0], pad=9, max_new=9) == SENTINEL).all())
+    assert bool((run_prefill(cfg, q, q[:, :2], q[:, :2], [0, 0, 0], pad=9, max_new=9) == SENTINEL).all())
+
+
+RANDOM = range(int(os.environ.get("FIER_RANDOM_PROMPT_SEEDS", "24")))
+
+
+def random_shape(seed):
+    rng = np.random.default_rng(seed)
+    hkv = int(rng.choice([1, 2, 3, 5]))
+    return rng, int(rng.integers(1, 7)), hkv * int(rng.integers(1, 9)), hkv, int(rng.choice([F16, BF16]))
+
+
+def edges(rng, most, n):
+    """Lengths: around multiples of 32, of 64 and of 96, small ones, anything."""
+    kind = rng.integers(0, 4, n)
+    near = rng.choice([32, 64, 96, 128], n) * rng.integers(0, 8, n) + rng.integers(-1, 2, n)
+    x = np.where(kind == 0, near, np.where(kind == 1, rng.integers(0, 4, n), rng.integers(0, most + 1, n)))
+    return np.clip(x, 0, most)
+
+
+@pytest.mark.parametrize("seed", RANDOM)
+def test_random_prompts(seed):
+    rng, nb, hq, hkv, dtype = random_shape(seed)
+    lens = edges(rng, 500, nb).tolist()
+    n = sum(lens)
+    cfg = B.make_config(nb, hq, hkv, 512, dtype, sm_scale=float(rng.choice([0.0884, 0.02, -0.05])))
+    q, k, v = randn((n, hq, D), dtype, 3 * seed + 1), randn((n, hkv, D), dtype, 3 * seed + 2), randn((n, hkv, D), dtype, 3 * seed + 3)
+    out = run_prefill(cfg, q, k, v, lens, pad=int(rng.integers(0, 3)), max_new=max(lens) + int(rng.integers(0, 50)), fused=bool(seed % 2))
+    check_prefill(out, q, k, v, lens, cfg.sm_scale)
+
+
+@pytest.mark.parametrize("seed", RANDOM)
+def test_random_chunks(seed):
+    rng, nb, hq, hkv, dtype = random_shape(1000 + seed)
+    most = int(rng.choice([1, 4, 40, 300]))
+    new = edges(rng, most, nb).tolist()
+    new[-1] = max(1, new[-1])
+    first = edges(rng, int(rng.choice([300, 4000])), nb).tolist()
+    g = int(rng.choice([32, 128]))
+    bt = int(rng.choice([0, 128, 256]))
+    cap = -(-max(f + n for f, n in zip(first, new)) // 256) * 256 + 256 * int(rng.integers(0, 2))
+    cfg = B.make_config(nb, hq, hkv, cap, dtype, group_size=g)
+    rows, cache = make_cache(cfg, first, new, dtype, bt, 5000 + 50 * seed)
+    q = randn((sum(new), hq, D), dtype, 6000 + seed)
+    pad = int(rng.integers(0, 3))
+    ws = B.make_chunk_workspace(cfg, sum(new) + pad, max(new) + 3)
+    for _ in range(2):
+        out = run_chunk(cfg, cache, q, new, pad=pad, ws=ws, max_new=max(new) + 3)
+        check_chunk(out, q, rows, first, new, cfg)
+
+
+# ---- addresses beyond 32 bits ------------------------------------------------------------------------------------------------
+
+
+def attention64_gpu(q, k, v, first, scale):
+    """One head, a query row at a time: (outputs, tolerances) as attention64's."""
+    o, t = [], []
+    u = torch.finfo(q.dtype).eps / 2
+    for i in range(q.shape[0]):
+        x = q[i].double()
+        kk, vv = k[: first + i + 1].double(), v[: first + i + 1].double()
+        w = torch.softmax(scale * (kk @ x), dim=0)
+        a = float((kk.abs() @ x.abs()).max()) * abs(scale)
+        y = w @ vv
+        o.append(y)
+        t.append((u + 2 * 132 * 2.0**-24 * a + 1e-5) * (w @ vv.abs()) * 1.01 + u * y.abs() + 2.0**-24 + 2.0**-32 * vv.abs().sum(dim=0))
+    return torch.stack(o).cpu(), torch.stack(t).cpu()
+
+
+def test_a_cache_of_more_than_four_gigabytes():
+    """Two sequences of 2^20 rows, 8 kv heads: 4.3 GB each of K and V.  Chunks into the last rows, attention over all of them."""
+    cfg = B.make_config(2, 8, 8, 1 << 20, BF16)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    k, v = (torch.empty(16, 1 << 20, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (k, v):
+        for u in range(16):
+            t[u] = torch.randn((1 << 20, D), generator=gen, device="cuda")
+    first, new = [7, (1 << 20) - 5], [2, 5]
+    cache = B.DeviceCache(cfg, k, v, i32(first))
+    x = randn((7, 24, D), BF16, 91).cuda()
+    starts = i32(starts_of(new))
+    B.append_chunk(cfg, cache, x[:, 8:16], x[:, 16:], starts, 5)
+    out = torch.zeros(7, 8, D, dtype=torch.bfloat16, device="cuda")
+    B.chunk_attn(cfg, cache, x[:, :8], starts, 5, out, B.make_chunk_workspace(cfg, 7, 5))
+    torch.cuda.synchronize()
+    for h in (0, 7):
+        assert torch.equal(k[8 + h, -5:], x[2:, 8 + h]) and torch.equal(v[8 + h, -5:], x[2:, 16 + h])
+        assert torch.equal(k[h, 7:9], x[:2, 8 + h])
+        for b, at in ((0, 0), (1, 2)):
+            want, tol = attention64_gpu(x[at:at + new[b], h], k[8 * b + h], v[8 * b + h], first[b], cfg.sm_scale)
+            check_attention(out[at:at + new[b], h], want, tol, f"sequence {b} head {h}")
+
+
+def test_a_pool_of_more_than_four_gigabytes():
+    cfg = B.make_config(1, 8, 8, 1024, F16)
+    n_pool = (1 << 32) // (8 * 64 * D * 2) + 40  # blocks of 64 rows of 8 heads
+    k, v = (torch.empty(n_pool, 8, 64, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    table = torch.arange(n_pool - 16, n_pool, dtype=torch.int32).flip(0).view(1, 16).contiguous()
+    for t in (k, v):
+        t[table[0].long().cuda()] = float("nan")
+    cache = B.DeviceCache(cfg, k, v, i32([0]), table.cuda())
+    x = randn((700, 24, D), F16, 92)
+    xd, starts = x.cuda(), i32([0, 700])
+    B.append_chunk(cfg, cache, xd[:, 8:16], xd[:, 16:], starts, 700)
+    out = torch.zeros(700, 8, D, dtype=torch.float16, device="cuda")
+    B.chunk_attn(cfg, cache, xd[:, :8], starts, 700, out, B.make_chunk_workspace(cfg, 700, 700))
+    torch.cuda.synchronize()
+    want, tol = attention64(x[:, :8], x[:, 8:16], x[:, 16:], 0, cfg.sm_scale)
+    check_attention(out, want, tol)
+
+
+def test_tokens_far_apart():
+    """Rows 2^23 elements apart, the last of them more than 4 GB from the first."""
+    n, stride = 270, 1 << 23
+    cfg = B.make_config(2, 2, 1, 512, BF16)
+    mem = torch.empty((n - 1) * stride + 4 * D, dtype=torch.bfloat16, device="cuda")
+    x = mem.as_strided((n, 4, D), (stride, D, 1))
+    host = randn((n, 4, D), BF16, 93)
+    x.copy_(host)
+    lens = [200, 70]
+    out = torch.zeros(n, 2, D, dtype=torch.bfloat16, device="cuda")
+    B.prefill_attn(cfg, x[:, :2], x[:, 2:3], x[:, 3:], i32(starts_of(lens)), 200, out)
+    cache = make_cache(cfg, [0, 0], [0, 0], BF16, 0, 94)[1]
+    B.append_chunk(cfg, cache, x[:, 2:3], x[:, 3:], i32(starts_of(lens)), 200)
+    torch.cuda.synchronize()
+    at = 0
+    for b, m in enumerate(lens):
+        want, tol = attention64(host[at:at + m, :2], host[at:at + m, 2:3], host[at:at + m, 3:], 0, cfg.sm_scale)
+        check_attention(out[at:at + m], want, tol)
+        assert torch.equal(cache.k[b, :m].cpu(), host[at:at + m, 2]) and torch.equal(cache.v[b, :m].cpu(), host[at:at + m, 3])
+        at += m
