@@ -363,8 +363,8 @@ __device__ __forceinline__ void join_partials(const float* slots, size_t pitch, 
 constexpr int kSideTile = 32;    // rows of K and V per wavefront and step side by side
 constexpr int kSideWaves = 3;    // of the four: so three such workgroups fit a CU's LDS
 constexpr int kSideStep = kSideWaves * kSideTile;
-constexpr int kSideLeast = 2;    // steps of a part, at least
-constexpr int kSharedLeast = 8;  // steps of 64 rows of a part of shared rows, at least
+constexpr int kSideLeast = 1;    // steps of a part, at least
+constexpr int kSharedLeast = 2;  // steps of 64 rows of a part of shared rows, at least
 // Parts of a tile, at most.  Side by side, up to 8 are joined by the last of their workgroups; more in groups of up to 7 by the last of
 // each, and the groups by the last of those: eight counters.  Up to 64 steps are not worth the second round: 2 x 2000 tokens, 8 kv heads
 // 16.0 us in 11 parts, 12.0 in 8.

@@ -203,6 +203,17 @@ def test_block_table_lengths_out_of_range_and_few_slots():
     check_table(cfg, 64, [10, 300, -3], [-1, -5, -9], table, free, 9)
 
 
+def test_block_table_of_the_largest_batch():
+    """16384 sequences: their sums fill 64 KiB of shared memory."""
+    n = 16384
+    rng = np.random.default_rng(5)
+    old, new = rng.integers(0, 257, n), rng.integers(0, 257, n)
+    cfg = B.make_config(n, 1, 1, 256, F16)
+    spare = max(0, int((-(-new // 64) + old // -64).sum())) + 7
+    table, free = table_case(n, 256, 64, old, spare, 6)
+    check_table(cfg, 64, old, new, table, free, spare)
+
+
 def test_block_table_without_offsets():
     cfg = B.make_config(2, 1, 1, 256, F16)
     table, free = table_case(2, 256, 64, [10, 64], 4, 2)
