@@ -8,6 +8,7 @@
  *   2. score every cached token: q . dequant(1-bit key)           (Alg. 1 step 2)
  *   3. pick the top-B tokens per kv head                          (Alg. 1 step 3)
  *   4. exact softmax attention over the selected K/V rows only    (Alg. 1 step 4)
+ * and what brings tokens into its caches: attention of prompts and chunks, their append, block tables.
  *
  * General rules of this ABI
  *   - Plain C.  Every pointer in fier_cache and every pointer argument documented as

@@ -612,7 +612,7 @@ struct SharedTile {
 
 // ---- shared tiles in several parts: a second launch joins them ------------------------------------------------------------------
 // Joined by the last workgroup of each tile, as the side-by-side ones are, it was one CU that read up to 3 MB: 64 tokens of 32 q / 8 kv
-// heads behind 32768 took 93 us, now 62.
+// heads behind 32768 took 93 us, now 62 to 69.
 // Per wavefront o as the lanes hold it, 16 chunks of 64 x 4 floats (channel tile ct, channels 8 i + 4 h + 0..3: chunk 4 ct + i),
 // then m and l of the lanes.
 __device__ __forceinline__ float* shared_slot(const PromptArgs& a, const Item& it, int head, int turned, int part) {
@@ -704,7 +704,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
 // one is loaded a step ahead, and one of V, loaded during the step's first logits.  48 KiB and at most 168 registers, so that
 // three workgroups share a CU and one's products run beside another's exponentials.
 //   What bounds it: power.  At 16384 tokens of 32 heads (2.09 ms, 1.05 PFLOP/s; a large library product of random numbers makes
-// 1.2) the matrix cores are busy 56 % of the cycles, at 1.6 GHz.  Two workgroups per CU with twice the registers, each
+// 1.2) the matrix cores are busy 62 % of the cycles, at 1.6 GHz; without the softmax the loop runs at 1.22.  Two workgroups per CU with twice the registers, each
 // wavefront's exponentials interleaved with its next products, were busy 50 % at 1.74 GHz: 2.30 ms.  64 rows a wavefront
 // (half the LDS reads) needs accumulation registers and the moves to and from them: 2.83.  Fewer instructions pay: addresses in
 // registers instead of made anew 2.16 -> 2.09.
