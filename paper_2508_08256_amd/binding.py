@@ -400,12 +400,19 @@ def _whole(t, heads: int, head_dim: int, n: int, what: str):
     return _rows(t, heads, head_dim, n, what)[0]
 
 
+def _offsets(cfg: Config, starts):
+    """The pointer of [batch + 1] int32 (a sum that torch forms has 64 bits)."""
+    if starts.numel() <= cfg.batch or starts.element_size() != 4 or not starts.is_contiguous():
+        raise FierError(ESHAPE, f"starts: {tuple(starts.shape)} of {starts.dtype}, {cfg.batch + 1} int32 are wanted")
+    return starts.data_ptr()
+
+
 def prefill_attn(cfg: Config, q, k, v, starts, max_new: int, out):
     """q, out [n_tokens][n_q_heads][128], k, v [n_tokens][n_kv_heads][128] (out contiguous, the others may be views of a fused
     projection); starts [batch + 1] int32."""
     n, d, hq, hkv = q.size(0), cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads
     _check(lib().fier_prefill_attn(C.byref(cfg), *_rows(q, hq, d, n, "q"), *_rows(k, hkv, d, n, "k"), *_rows(v, hkv, d, n, "v"),
-                                   _ptr(starts), n, int(max_new), _whole(out, hq, d, n, "out"), _stream()),
+                                   _offsets(cfg, starts), n, int(max_new), _whole(out, hq, d, n, "out"), _stream()),
            "fier_prefill_attn")
 
 
@@ -424,7 +431,7 @@ def make_chunk_workspace(cfg: Config, n_tokens: int, max_new: int):
 
 def chunk_attn(cfg: Config, cache: DeviceCache, q, starts, max_new: int, out, workspace):
     n, d, hq = q.size(0), cfg.head_dim, cfg.n_q_heads
-    _check(lib().fier_chunk_attn(C.byref(cfg), C.byref(cache.c), *_rows(q, hq, d, n, "q"), _ptr(starts), n, int(max_new),
+    _check(lib().fier_chunk_attn(C.byref(cfg), C.byref(cache.c), *_rows(q, hq, d, n, "q"), _offsets(cfg, starts), n, int(max_new),
                                  _whole(out, hq, d, n, "out"), *_ws(workspace), _stream()), "fier_chunk_attn")
 
 
@@ -432,7 +439,7 @@ def append_chunk(cfg: Config, cache: DeviceCache, k_new, v_new, starts, max_new:
     """k_new, v_new [n_tokens][n_kv_heads][128], possibly views; starts [batch + 1] int32."""
     n, d, hkv = k_new.size(0), cfg.head_dim, cfg.n_kv_heads
     _check(lib().fier_append_chunk(C.byref(cfg), C.byref(cache.c), *_rows(k_new, hkv, d, n, "k_new"),
-                                   *_rows(v_new, hkv, d, n, "v_new"), _ptr(starts), n, int(max_new), _stream()),
+                                   *_rows(v_new, hkv, d, n, "v_new"), _offsets(cfg, starts), n, int(max_new), _stream()),
            "fier_append_chunk")
 
 

@@ -129,3 +129,18 @@ def test_the_binding_refuses_other_layouts(monkeypatch):
         args[at] = bad
         with pytest.raises(B.FierError):
             B.block_table(cfg, 64, *args)
+
+
+@pytest.mark.parametrize("starts", [torch.zeros(3, dtype=torch.int64), torch.zeros(2, dtype=torch.int32),
+                                    torch.zeros(6, dtype=torch.int32)[::2]])
+def test_the_binding_refuses_other_offsets(monkeypatch, starts):
+    """torch's sums of int32 lengths have 64 bits: read as 32-bit offsets they would be other sequences."""
+    monkeypatch.setattr(B, "_stream", lambda: None)
+    cfg, cache = B.make_config(2, 4, 2, 256, B.BF16), types.SimpleNamespace(c=CACHE)
+    q, k = torch.zeros(10, 4, 128, dtype=torch.bfloat16), torch.zeros(10, 2, 128, dtype=torch.bfloat16)
+    ws = torch.zeros(64, dtype=torch.uint8)
+    for call in (lambda: B.prefill_attn(cfg, q, k, k, starts, 0, q), lambda: B.append_chunk(cfg, cache, k, k, starts, 0),
+                 lambda: B.chunk_attn(cfg, cache, q, starts, 0, q, ws)):
+        with pytest.raises(B.FierError) as e:
+            call()
+        assert e.value.status == B.ESHAPE
