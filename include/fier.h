@@ -281,11 +281,13 @@ int fier_decode_step_phase(const fier_config *cfg, const fier_cache *layers, int
  *   n_tokens (host) rows of the arrays, at most 2^24;  max_new (host): a bound on the new tokens of any one sequence;
  *            those past it are left out.  Both may be 0
  *   q        [n_tokens][n_q_heads][D], k, v, k_new, v_new [n_tokens][n_kv_heads][D], device, K dtype.  Each has a stride:
- *            the ELEMENTS from a token to the next, a multiple of 8 and at least heads * D (FIER_EALIGN, FIER_ESHAPE),
- *            so that views of one fused projection can be passed as they are
+ *            the ELEMENTS from a token to the next, a multiple of 8 (FIER_EALIGN), at least heads * D and at most 2^24
+ *            (FIER_ESHAPE), so that views of one fused projection can be passed as they are
  *   out      [n_tokens][n_q_heads][D] in the K DTYPE (a prompt's outputs feed 16-bit products), device, contiguous
  * Logits, softmax and sums are binary32; the weights are rounded to the K dtype for the product with V (to nearest, relative
  * to a sum that is not), the outputs once at the end.  sm_scale must be finite (any sign).  Integer arrays are 4-byte aligned.
+ * k and v must be finite as K and V are: a value of v that is not reaches the outputs of tokens in front of it too, since it
+ * meets their weights of 0.  Logits and 256 times the sum of |v| over a sequence's rows must lie within binary32.
  */
 
 /* Causal attention of whole prompts: token i of a sequence attends over its tokens 0 .. i.  No cache and no workspace.  Of

@@ -704,10 +704,10 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
 // one is loaded a step ahead, and one of V, loaded during the step's first logits.  48 KiB and at most 168 registers, so that
 // three workgroups share a CU and one's products run beside another's exponentials.
 //   What bounds it: power.  At 16384 tokens of 32 heads (2.09 ms, 1.05 PFLOP/s; a large library product of random numbers makes
-// 1.2) the matrix cores are busy 62 % of the cycles, at 1.6 GHz; without the softmax the loop runs at 1.22.  Two workgroups per CU with twice the registers, each
-// wavefront's exponentials interleaved with its next products, were busy 50 % at 1.74 GHz: 2.30 ms.  64 rows a wavefront
-// (half the LDS reads) needs accumulation registers and the moves to and from them: 2.83.  Fewer instructions pay: addresses in
-// registers instead of made anew 2.16 -> 2.09.
+// 1.2) the matrix cores are busy 62 % of the cycles, at 1.6 GHz; without the softmax the loop runs at 1.22.  Two workgroups per
+// CU with twice the registers, each wavefront's exponentials interleaved with its next products, were busy 50 % at 1.74 GHz:
+// 2.30 ms.  64 rows a wavefront (half the LDS reads) needs accumulation registers and the moves to and from them: 2.83.  Fewer
+// instructions pay: addresses in registers instead of made anew 2.16 -> 2.09.
 template <int DT, bool CACHE>
 __device__ __forceinline__ void attend_shared(const PromptArgs& a, const Item& it, int head, lds_char* lds) {
   const PromptSpan sp = it.sp;
