@@ -324,8 +324,12 @@ int fier_append_chunk(const fier_config *cfg, const fier_cache *cache, const voi
  *               growing sequence's new entries are filled in; the others are left as they are
  *   free_blocks [n_blocks]: the free blocks of the pool, a stack of *n_free.  What sequences give back is pushed (sequences,
  *               then entries ascending), what they need popped afterwards (in the same order)
- *   n_free_out  (not n_free) receives how many are free afterwards.  If that is negative there are as many too few: then
- *               nothing else is written
+ *   n_free_out  (not n_free) receives how many are free afterwards.  If that is negative there are as many too few, and the
+ *               step has not taken place: table, free_blocks and slots stay as they are, and every entry of starts becomes
+ *               starts[0], so that no sequence has tokens in the calls enqueued behind this one.  old_lens and *n_free
+ *               hold on: repeat the call from them once there are blocks.  A negative *n_free is passed on as it is, with the
+ *               same effect.  (Lengths that grow by starts[b + 1] - starts[b] on the GPU stay right.  The decode step takes
+ *               no offsets: enqueue one behind a call only if it cannot fall short, or after n_free_out has been read)
  *   starts      optional [batch + 1]: packed offsets of the tokens by which sequences grow, as the calls above take them
  *   slots       optional (with starts) [n_slots]: for every such token the row table[...] * block_tokens + position in the
  *               block; those past n_slots are left out, further entries left as they are

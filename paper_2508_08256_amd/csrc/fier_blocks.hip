@@ -16,6 +16,9 @@ constexpr int kTableEntries = 256;  // entries of a sequence per workgroup, one 
 // takes a block that another sequence gives back in this call from that sequence's old entries, which no workgroup changes.
 // Entries of the table are written only past a growing sequence's old ones and places of the stack only from n on, while only
 // those below n are read: the call can be repeated on its own results.
+//   Too few blocks: the calls enqueued behind this one must not write through entries that nobody filled, so all offsets become
+// starts[0], which only this case reads and no case but a successful one writes: then no sequence has new tokens.  A negative
+// counter says the same of the call before: it is passed on, not taken for an empty stack.
 __global__ __launch_bounds__(256) void block_table_kernel(int shift, int max_ctx, int batch, const int32_t* __restrict__ old_lens,
                                                           const int32_t* __restrict__ new_lens, int32_t* table,
                                                           int32_t* free_blocks, int n_blocks,
@@ -45,9 +48,16 @@ __global__ __launch_bounds__(256) void block_table_kernel(int shift, int max_ctx
 #pragma unroll
   for (int k = 0; k < 5; ++k) sum[k] = part[k][0] + part[k][1] + part[k][2] + part[k][3];
   const int take_before = (int)sum[0], give_before = (int)sum[1], tok_before = (int)sum[2];
-  const int T = (int)sum[3], R = (int)sum[4], n = max(0, min(*n_free, n_blocks)), left = n + R - T;
+  const int T = (int)sum[3], R = (int)sum[4], n = min(*n_free, n_blocks), left = n < 0 ? n : n + R - T;
   if (b == 0 && blockIdx.y == 0 && tid == 0) *n_free_out = left;
-  if (left < 0) return;
+  if (left < 0) {
+    if (starts && blockIdx.y == 0 && tid == 0) {
+      const int none = starts[0];
+      if (b > 0) starts[b] = none;
+      if (b == batch - 1) starts[batch] = none;
+    }
+    return;
+  }
   const int o = clamped(old_lens[b]), w = clamped(new_lens[b]);
   if (starts && blockIdx.y == 0 && tid == 0) {
     starts[b] = tok_before;
