@@ -281,12 +281,20 @@ struct Rows32 {
   }
 };
 
+// Two outputs.  A mean of V lies within V's type, but rounded weights over a sum that is not can make it larger by 2^-11 (fp16):
+// past 65520 it would become an infinity.  (bf16 values that large are outside what the sums can hold.)
+template <int DT>
+__device__ __forceinline__ uint32_t pack2_outputs(float a, float b) {
+  constexpr float kMost = 65504.f;
+  if (DT == DT_F16) return pack2<DT>(__builtin_amdgcn_fmed3f(a, -kMost, kMost), __builtin_amdgcn_fmed3f(b, -kMost, kMost));
+  return pack2<DT>(a, b);
+}
 template <int DT>
 __device__ __forceinline__ void store_channels(char* out_row, int ct, int h, const floatx16_t& o, float inv) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     *reinterpret_cast<uint2*>(out_row + ct * 64 + i * 16 + h * 8) =
-        make_uint2(pack2<DT>(o[4 * i] * inv, o[4 * i + 1] * inv), pack2<DT>(o[4 * i + 2] * inv, o[4 * i + 3] * inv));
+        make_uint2(pack2_outputs<DT>(o[4 * i] * inv, o[4 * i + 1] * inv), pack2_outputs<DT>(o[4 * i + 2] * inv, o[4 * i + 3] * inv));
 }
 
 // ---- one query row per lane and half ------------------------------------------------------------------------------------
@@ -679,7 +687,7 @@ __device__ __forceinline__ void join_chunks(const PromptArgs& a, const Item& it,
 #pragma unroll
       for (int x = 0; x < CH; ++x)
         *reinterpret_cast<uint2*>(row.out + ((c & 15) + x) * 16 + (lane >> 5) * 8) =
-            make_uint2(pack2<DT>(o[x][0] * inv, o[x][1] * inv), pack2<DT>(o[x][2] * inv, o[x][3] * inv));
+            make_uint2(pack2_outputs<DT>(o[x][0] * inv, o[x][1] * inv), pack2_outputs<DT>(o[x][2] * inv, o[x][3] * inv));
     }
   }
 }
