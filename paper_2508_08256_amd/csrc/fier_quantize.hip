@@ -215,6 +215,10 @@ __device__ __forceinline__ uint32_t transpose_nibbles(uint32_t v, uint32_t sel4,
   return (v & keep1) | (o & ~keep1);
 }
 
+// Workgroups of a chunk's append along x, the rest along y: a dimension holds fewer than 2^32 threads, and a loose bound on the
+// chunks of many sequences with long caches is more (8192 units, 131072 tokens: 4.6e9).
+constexpr unsigned kGridX = 1u << 20;
+
 // Whole groups, and the partial one at a unit's end.  Grid units * (1 + n_x), n_x >= ceil(n_pairs / (4 bpw)), block 256.
 // The first `units` workgroups do the units' partial groups (the longest chain of dependent loads:
 // started last it would end the kernel late, and as a kernel of its own it took 4 to 17 us after this one); then wave w
@@ -248,9 +252,10 @@ __global__ __launch_bounds__(256, 4) void quantize_kernel(uint32_t* __restrict__
   // compiler too
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n_quant = units * (1 + n_x);
-  const int wid = (int)blockIdx.x - units;
-  const int unit = kNew && (int)blockIdx.x >= n_quant ? ((int)blockIdx.x - n_quant) / src.n_copy
-                                                      : (wid < 0 ? (int)blockIdx.x : wid / n_x);
+  const int item = kNew ? (int)(blockIdx.y * kGridX + blockIdx.x) : (int)blockIdx.x;
+  if (kNew && item >= n_quant + units * src.n_copy) return;
+  const int wid = item - units;
+  const int unit = kNew && item >= n_quant ? (item - n_quant) / src.n_copy : (wid < 0 ? item : wid / n_x);
   int L = seq_lens[unit / n_kv_heads];
   L = L < 0 ? 0 : (L > max_ctx ? max_ctx : L);
   const int L0 = L;  // tokens in the cache before a chunk
@@ -266,9 +271,9 @@ __global__ __launch_bounds__(256, 4) void quantize_kernel(uint32_t* __restrict__
     n_full = NS == 1 ? L / kPair : (L / (kG * NS)) * (NS / 2);
     kn = src.k + (int64_t)(lo - L0) * src.k_stride + head * (kD * 2);
     vn = src.v + (int64_t)(lo - L0) * src.v_stride + head * (kD * 2);
-    if ((int)blockIdx.x >= n_quant) {
+    if (item >= n_quant) {
       // 64 tokens of V: token t0 + 16 i + 4 wave + lane / 16, a multiple of 64 at the start
-      const int t0 = (L0 / kPair + ((int)blockIdx.x - n_quant) % src.n_copy) * kPair;
+      const int t0 = (L0 / kPair + (item - n_quant) % src.n_copy) * kPair;
       if (t0 >= L) return;
       auto load = [&](const char* rows, int64_t stride, uint4 (&w)[4]) {
 #pragma unroll
@@ -519,7 +524,9 @@ template <int DT, class Rows>
 static void launch_quantize_dt(KvLayout lay, uint32_t* K, uint32_t* kbits, uint32_t* kmeta, float* kabsmax,
                                const int32_t* seq_lens, int units, int n_kv_heads, int max_ctx, int ns, int bpw, int n_x,
                                int n_copy, Rows src, hipStream_t st) {
-  const dim3 grid((unsigned)units * (unsigned)(1 + n_x + n_copy));
+  // at most 65535 units of 1 + 1025 + 16384 workgroups: 32 bits hold them
+  const unsigned all = (unsigned)units * (unsigned)(1 + n_x + n_copy);
+  const dim3 grid(n_copy ? std::min(all, kGridX) : all, n_copy ? (all + kGridX - 1) / kGridX : 1);
 #define FIER_Q_CASE(NS)                                                                                               \
   quantize_kernel<DT, NS, Rows><<<grid, 256, 0, st>>>(K, kbits, kmeta, kabsmax, seq_lens, units, n_kv_heads, max_ctx, \
                                                       bpw, n_x, lay, src)
