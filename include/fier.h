@@ -285,7 +285,8 @@ int fier_decode_step_phase(const fier_config *cfg, const fier_cache *layers, int
  *            (FIER_ESHAPE), so that views of one fused projection can be passed as they are
  *   out      [n_tokens][n_q_heads][D] in the K DTYPE (a prompt's outputs feed 16-bit products), device, contiguous
  * Logits, softmax and sums are binary32; the weights are rounded to the K dtype for the product with V (to nearest, relative
- * to a sum that is not), the outputs once at the end.  sm_scale must be finite (any sign).  Integer arrays are 4-byte aligned.
+ * to a sum that is not), the outputs once at the end.  sm_scale may have any sign; sm_scale * log2(e) must be finite in
+ * binary32 (FIER_EINVAL).  Integer arrays are 4-byte aligned.
  * k and v must be finite as K and V are: a value of v that is not reaches the outputs of tokens in front of it too, since it
  * meets their weights of 0.  Logits and 256 times the sum of |v| over a sequence's rows must lie within binary32.
  */

@@ -603,6 +603,8 @@ static int check_new(const fier_config* cfg, const int32_t* starts, int32_t n_to
   return n_tokens > kMaxNewTokens ? FIER_ESHAPE : FIER_OK;
 }
 
+// The kernel's scale, of powers of two.  Infinite from an sm_scale of 2.36e38 on: a logit of 0 would become a NaN.
+static float prompt_scale(const fier_config* cfg) { return std::fabs(cfg->sm_scale) * 1.4426950408889634f; }
 static fier::PromptArgs prompt_args(const fier_config* cfg, const void* q, int64_t q_stride, const int32_t* starts,
                                     int32_t n_tokens, int32_t max_new, void* out) {
   fier::PromptArgs a = {};
@@ -610,8 +612,8 @@ static fier::PromptArgs prompt_args(const fier_config* cfg, const void* q, int64
   a.out = static_cast<char*>(out);
   a.q_stride = 2 * q_stride;
   a.starts = starts;
-  // scale = |sm_scale| log2(e); the sign goes to the queries, and a scale of zero makes them zero
-  a.scale = cfg->sm_scale == 0.f ? 1.f : std::fabs(cfg->sm_scale) * 1.4426950408889634f;
+  // the sign goes to the queries, and a scale of zero makes them zero
+  a.scale = cfg->sm_scale == 0.f ? 1.f : prompt_scale(cfg);
   a.flip = cfg->sm_scale < 0.f ? 0x80008000u : 0u;
   a.keep = cfg->sm_scale == 0.f ? 0u : 0xffffffffu;
   a.batch = cfg->batch;
@@ -634,7 +636,7 @@ int fier_prefill_attn(const fier_config* cfg, const void* q, int64_t q_stride, c
                       void* stream) {
   int st = check_new(cfg, starts, n_tokens, max_new);
   if (st != FIER_OK) return st;
-  if ((n_tokens && (!q || !k || !v || !out)) || !std::isfinite(cfg->sm_scale)) return FIER_EINVAL;
+  if ((n_tokens && (!q || !k || !v || !out)) || !std::isfinite(prompt_scale(cfg))) return FIER_EINVAL;
   if (misaligned(out)) return FIER_EALIGN;
   for (int rc : {check_rows(q, q_stride, cfg->n_q_heads), check_rows(k, k_stride, cfg->n_kv_heads),
                  check_rows(v, v_stride, cfg->n_kv_heads)})
@@ -651,7 +653,7 @@ int fier_chunk_attn(const fier_config* cfg, const fier_cache* cache, const void*
   if (st != FIER_OK) return st;
   st = check_cache(cfg, cache);
   if (st != FIER_OK) return st;
-  if ((n_tokens && (!q || !out)) || !std::isfinite(cfg->sm_scale)) return FIER_EINVAL;
+  if ((n_tokens && (!q || !out)) || !std::isfinite(prompt_scale(cfg))) return FIER_EINVAL;
   if (misaligned(out)) return FIER_EALIGN;
   st = check_rows(q, q_stride, cfg->n_q_heads);
   if (st != FIER_OK) return st;
