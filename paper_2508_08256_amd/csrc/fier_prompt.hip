@@ -249,7 +249,7 @@ struct Rows32 {
       l *= alpha;
 #pragma unroll
       for (int ct = 0; ct < 4; ++ct) o[ct] *= alpha;
-      large = __any(fabsf(m) >= kLargeScaled);
+      large = __any(fabsf(m) >= kLargeScaled && m != -FLT_MAX);  // not a row that has met no token yet
     }
     // The weights take the scaled logit unrounded, which is the more accurate while logits are small.  From 2^22 on its
     // distance from the rounded maximum would be that one's rounding error: there both are rounded alike.

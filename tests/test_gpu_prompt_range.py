@@ -40,3 +40,29 @@ def test_the_mean_of_the_largest_values_is_finite(first, new, n_q):
         out = run_chunk(cfg, B.DeviceCache(cfg, *dev, i32([first])), q, [new])
     # the true output, and 1 + 2^-11 more of it held to the largest; binary32 is off by far less than half a step, 16
     assert torch.equal(out.double(), (65504.0 * sign.double()).expand(new, n_q, D))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("first,new,edge", [(30, 8, 32), (100, 200, 128)])
+def test_rows_without_a_token_so_far_do_not_round_the_logits_of_others(dtype, first, new, edge):
+    """Scaled logits just below 2^22, (2^22 + 0..3) * 0.6 * log2(e) = 3.6e6 and exact before the scale: unrounded they give weights
+    within 1e-5, rounded by themselves (the form for larger ones) within 8 % only.  Of the tokens from `edge` on, whose
+    wavefront begins there, the first rows see none.  Column d + 4 (token past the edge) of v is 1 for the tokens of logit d: outputs
+    are sums of weights of one sign, off by their roundings (u each of the weights and the output, half a step) and those 1e-5."""
+    rows = first + new
+    cap = -(-rows // 64) * 64
+    cfg = B.make_config(1, 1, 1, cap, dtype, sm_scale=0.6)
+    j = torch.arange(rows)
+    q, k, v = (torch.zeros(n, 1, D, dtype=torch.float64) for n in (new, rows, rows))
+    q[:, 0, 0], q[:, 0, 1] = 2048, 1
+    k[:, 0, 0], k[:, 0, 1] = 2048, (j % 4).double()
+    v[j, 0, j % 4 + 4 * (j >= edge)] = 1
+    q, k, v = (t.to(torch.float16 if dtype == F16 else torch.bfloat16) for t in (q, k, v))
+    dev = [torch.zeros(1, cap, D, dtype=q.dtype, device="cuda") for _ in range(2)]
+    for d, s in zip(dev, (k, v)):
+        d[0, :rows] = s[:, 0].cuda()
+    out = run_chunk(cfg, B.DeviceCache(cfg, *dev, i32([first])), q, [new])[:, 0].double()
+    seen = j[None, :] <= first + torch.arange(new)[:, None]
+    want = torch.softmax(torch.where(seen, cfg.sm_scale * (j % 4).double(), -math.inf), dim=1) @ v[:, 0].double()
+    u = torch.finfo(q.dtype).eps / 2
+    assert bool(((out - want).abs() <= (2 * u + u * u + 1e-5) * want).all()), float(((out - want) / want.clamp(min=1e-9)).abs().max())
