@@ -79,18 +79,22 @@ __device__ __forceinline__ uint2 lds_read_transposed(const lds_char* p) {
 // Written as assembly, with a wait count of its own (wait_loads): the compiler takes every read of LDS for one that may need the
 // loads just issued, and waited for the next tile's rows before this one's product.  Nothing is returned in a register.  The
 // instruction after a write of M0 may not use it yet.
-// STREAM: with the hint for data that is read once.
+// STREAM: with the hint for data that is read once.  (M0 is named as clobbered, so that an instruction of the compiler's own that
+// used it would set it anew; the compiler remarks that it does not save the register, which nobody asks it to.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <bool STREAM>
 __device__ __forceinline__ void load_rows_to_lds(const char* base, uint32_t off, const lds_char* dst) {
   if (STREAM)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"((uint32_t)(uintptr_t)dst), "v"(off),
                  "s"(base)
-                 : "memory");
+                 : "memory", "m0");
   else
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)dst), "v"(off),
                  "s"(base)
-                 : "memory");
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // until at most N of the wavefront's loads are under way
 template <int N>
 __device__ __forceinline__ void wait_loads() {
