@@ -383,37 +383,58 @@ def decode_step_phase(cfg: Config, caches, q, k_new, v_new, budgets, max_budget:
                                         *_ws(workspace), int(phase), _stream()), "fier_decode_step_phase")
 
 
-def _rows(t, heads: int, head_dim: int, n: int, what: str):
-    """(pointer, elements from a token to the next) of a tensor [n][heads][head_dim] whose tokens may lie apart."""
-    if t.shape == (n, heads, head_dim) and t.element_size() == 2:
+_types = None
+
+
+def _torch_types():
+    """torch's types of F16 rows, BF16 rows and whole numbers."""
+    global _types
+    if _types is None:
+        import torch
+
+        _types = (torch.float16, torch.bfloat16, torch.int32)
+    return _types
+
+
+def _rows(t, dtype, heads: int, head_dim: int, n: int, what: str):
+    """(pointer, elements from a token to the next) of a tensor [n][heads][head_dim] of the K dtype whose tokens may lie apart."""
+    if t.dtype is dtype and t.shape == (n, heads, head_dim):
         if t.is_contiguous():
             return t.data_ptr(), heads * head_dim
         s = t.stride()
         if s[2] == 1 and (heads == 1 or s[1] == head_dim):
             return t.data_ptr(), s[0] if n > 1 else heads * head_dim  # a single token's stride may be anything
-    raise FierError(ESHAPE, f"{what}: {tuple(t.shape)}, strides {t.stride()}, of {n} tokens")
+    raise FierError(ESHAPE, f"{what}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, of {n} tokens")
 
 
-def _whole(t, heads: int, head_dim: int, n: int, what: str):
+def _whole(t, dtype, heads: int, head_dim: int, n: int, what: str):
     if not t.is_contiguous():
         raise FierError(ESHAPE, f"{what}: not contiguous")
-    return _rows(t, heads, head_dim, n, what)[0]
+    return _rows(t, dtype, heads, head_dim, n, what)[0]
 
 
-def _offsets(cfg: Config, starts):
+def _offsets(cfg: Config, starts, int32):
     """The pointer of [batch + 1] int32 (a sum that torch forms has 64 bits)."""
-    if starts.numel() <= cfg.batch or starts.element_size() != 4 or not starts.is_contiguous():
+    if starts.numel() <= cfg.batch or starts.dtype is not int32 or not starts.is_contiguous():
         raise FierError(ESHAPE, f"starts: {tuple(starts.shape)} of {starts.dtype}, {cfg.batch + 1} int32 are wanted")
     return starts.data_ptr()
+
+
+def _host_memory(what: str):
+    """A kernel would fault on such an address."""
+    return FierError(EINVAL, f"{what}: all tensors must be on the GPU")
 
 
 def prefill_attn(cfg: Config, q, k, v, starts, max_new: int, out):
     """q, out [n_tokens][n_q_heads][128], k, v [n_tokens][n_kv_heads][128] (out contiguous, the others may be views of a fused
     projection); starts [batch + 1] int32."""
-    n, d, hq, hkv = q.size(0), cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads
-    _check(lib().fier_prefill_attn(C.byref(cfg), *_rows(q, hq, d, n, "q"), *_rows(k, hkv, d, n, "k"), *_rows(v, hkv, d, n, "v"),
-                                   _offsets(cfg, starts), n, int(max_new), _whole(out, hq, d, n, "out"), _stream()),
-           "fier_prefill_attn")
+    n, d, hq, hkv, types = q.size(0), cfg.head_dim, cfg.n_q_heads, cfg.n_kv_heads, _torch_types()
+    t = types[cfg.kv_dtype == BF16]
+    args = (*_rows(q, t, hq, d, n, "q"), *_rows(k, t, hkv, d, n, "k"), *_rows(v, t, hkv, d, n, "v"),
+            _offsets(cfg, starts, types[2]), n, int(max_new), _whole(out, t, hq, d, n, "out"))
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and starts.is_cuda and out.is_cuda):
+        raise _host_memory("fier_prefill_attn")
+    _check(lib().fier_prefill_attn(C.byref(cfg), *args, _stream()), "fier_prefill_attn")
 
 
 def chunk_workspace_bytes(cfg: Config, n_tokens: int, max_new: int) -> int:
@@ -430,30 +451,44 @@ def make_chunk_workspace(cfg: Config, n_tokens: int, max_new: int):
 
 
 def chunk_attn(cfg: Config, cache: DeviceCache, q, starts, max_new: int, out, workspace):
-    n, d, hq = q.size(0), cfg.head_dim, cfg.n_q_heads
-    _check(lib().fier_chunk_attn(C.byref(cfg), C.byref(cache.c), *_rows(q, hq, d, n, "q"), _offsets(cfg, starts), n, int(max_new),
-                                 _whole(out, hq, d, n, "out"), *_ws(workspace), _stream()), "fier_chunk_attn")
+    n, d, hq, types = q.size(0), cfg.head_dim, cfg.n_q_heads, _torch_types()
+    t = types[cfg.kv_dtype == BF16]
+    args = (*_rows(q, t, hq, d, n, "q"), _offsets(cfg, starts, types[2]), n, int(max_new), _whole(out, t, hq, d, n, "out"))
+    if workspace is not None and not workspace.is_cuda:
+        raise FierError(EWORKSPACE, "fier_chunk_attn: the workspace must be on the GPU")
+    if not (q.is_cuda and starts.is_cuda and out.is_cuda):
+        raise _host_memory("fier_chunk_attn")
+    _check(lib().fier_chunk_attn(C.byref(cfg), C.byref(cache.c), *args, *_ws(workspace), _stream()), "fier_chunk_attn")
 
 
 def append_chunk(cfg: Config, cache: DeviceCache, k_new, v_new, starts, max_new: int):
     """k_new, v_new [n_tokens][n_kv_heads][128], possibly views; starts [batch + 1] int32."""
-    n, d, hkv = k_new.size(0), cfg.head_dim, cfg.n_kv_heads
-    _check(lib().fier_append_chunk(C.byref(cfg), C.byref(cache.c), *_rows(k_new, hkv, d, n, "k_new"),
-                                   *_rows(v_new, hkv, d, n, "v_new"), _offsets(cfg, starts), n, int(max_new), _stream()),
-           "fier_append_chunk")
+    n, d, hkv, types = k_new.size(0), cfg.head_dim, cfg.n_kv_heads, _torch_types()
+    t = types[cfg.kv_dtype == BF16]
+    args = (*_rows(k_new, t, hkv, d, n, "k_new"), *_rows(v_new, t, hkv, d, n, "v_new"), _offsets(cfg, starts, types[2]), n,
+            int(max_new))
+    if not (k_new.is_cuda and v_new.is_cuda and starts.is_cuda):
+        raise _host_memory("fier_append_chunk")
+    _check(lib().fier_append_chunk(C.byref(cfg), C.byref(cache.c), *args, _stream()), "fier_append_chunk")
 
 
 def block_table(cfg: Config, block_tokens: int, old_lens, new_lens, table, free_blocks, n_free, n_free_out, starts=None,
                 slots=None):
     """int32 tensors on the GPU: old_lens, new_lens [batch], table [batch][max_ctx / block_tokens], free_blocks [pool blocks],
     n_free, n_free_out of one element, starts [batch + 1], slots of any size."""
+    int32, on_gpu = _torch_types()[2], True
     for t in (old_lens, new_lens, table, free_blocks, n_free, n_free_out, starts, slots):
-        if t is not None and not (t.is_contiguous() and t.element_size() == 4):
-            raise FierError(EINVAL, "fier_block_table: contiguous int32 tensors are wanted")
-    if (old_lens.numel() != cfg.batch or new_lens.numel() != cfg.batch or block_tokens < 1
-            or table.numel() != cfg.batch * (cfg.max_ctx // block_tokens)
-            or (starts is not None and starts.numel() < cfg.batch + 1)):
+        if t is not None:
+            if t.dtype is not int32 or not t.is_contiguous():
+                raise FierError(EINVAL, "fier_block_table: contiguous int32 tensors are wanted")
+            on_gpu = on_gpu and t.is_cuda
+    n = cfg.batch
+    if (old_lens.numel() != n or new_lens.numel() != n or block_tokens < 1
+            or table.numel() != n * (cfg.max_ctx // block_tokens)
+            or (starts is not None and starts.numel() <= n)):
         raise FierError(ESHAPE, "fier_block_table")
+    if not on_gpu:
+        raise _host_memory("fier_block_table")
     _check(lib().fier_block_table(C.byref(cfg), int(block_tokens), _ptr(old_lens), _ptr(new_lens), _ptr(table),
                                   _ptr(free_blocks), free_blocks.numel(), _ptr(n_free), _ptr(n_free_out), _ptr(starts),
                                   _ptr(slots), 0 if slots is None else slots.numel(), _stream()), "fier_block_table")
