@@ -76,3 +76,19 @@ def test_the_binding_refuses_tensors_in_host_memory(monkeypatch):
     with pytest.raises(B.FierError) as e:
         B.block_table(cfg, 64, *(torch.zeros(n, dtype=torch.int32) for n in (2, 2, 8, 9, 1, 1, 3, 4)))
     assert e.value.status == B.EINVAL
+
+
+@pytest.mark.parametrize("n_q,n_kv", [(1, 1), (8, 8), (12, 4), (32, 8), (7, 1), (8, 1), (64, 64), (800, 800)])
+@pytest.mark.parametrize("batch", [1, 16, 80])
+def test_a_chunk_workspace_serves_every_smaller_call(n_q, n_kv, batch):
+    """As make_chunk_workspace promises: never less for more rows or a wider bound, around 32 query rows (where tiles that share rows
+    begin), around tiles of 128 and around the most parts."""
+    cfg = B.make_config(batch, n_q, n_kv, 4096)
+    rep = n_q // n_kv
+    near = {x // rep + d for x in (0, 32, 128, 48 * 128) for d in (-1, 0, 1, 2)}
+    ns = sorted({n for n in near | {1, 2, batch, batch + 1, 100, 1000, 5000, 1 << 17, 1 << 24} if 0 <= n <= 1 << 24})
+    size = {(n, m): B.chunk_workspace_bytes(cfg, n, m) for n in ns for m in ns}
+    for n0, n1 in zip(ns, ns[1:]):
+        for m in ns:
+            assert 0 < size[n0, m] <= size[n1, m], (n0, n1, m)
+            assert size[m, n0] <= size[m, n1], (m, n0, n1)
