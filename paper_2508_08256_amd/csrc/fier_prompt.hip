@@ -382,9 +382,13 @@ constexpr int kSharedLeast = 2;  // steps of 64 rows of a part of shared rows, a
 // 16.0 us in 11 parts, 12.0 in 8.
 constexpr int kGroup = 8, kMostParts = 48;
 constexpr int kPartsWanted = 768;
-// From so many bytes of K and V on, side-by-side tiles are loaded with the streaming hint, as the other gathers do it: one token of 16
-// sequences of 8k-64k 528 / 484 us (2.8 GB, 5.9 TB/s), of 128k 114 / 104; 134 MB, which the last cache can hold, 42 / 46.
-constexpr float kStreamBytes = 64 << 20;
+// From so many bytes of K and V on, more than the last cache keeps, side-by-side tiles are loaded with the streaming hint.  One token, us
+// without / with it, the rows read by other calls in between and, in parentheses, by the same call before:
+//   1 sequence, 32 q / 8 kv heads      128 MiB 41.6 / 41.0 (35.3 / 38.2)   256 MiB 66.3 / 61.5 (55.5 / 60.0)   512 MiB 115 / 105 (114 / 103)
+//   8 sequences, 32 heads               64 MiB 25.7 / 28.4 (22.9 / 24.4)   128 MiB 38.0 / 39.6 (33.3 / 41.2)
+//                                      256 MiB 61.2 / 60.0 (52.1 / 62.9)   512 MiB 109 / 101 (110 / 101)
+// and 16 sequences of 8k-64k (2.8 GB) 528 / 484.
+constexpr float kStreamBytes = 256 << 20;
 constexpr unsigned kGridY = 32768;  // items along y, the rest along z
 
 struct SequenceWork {
