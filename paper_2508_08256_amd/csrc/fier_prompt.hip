@@ -456,10 +456,12 @@ __device__ __forceinline__ bool find_item(const PromptArgs& a, int j, int lane, 
     int64_t tokens = tokens0;
     for (int b0 = 64; b0 < a.batch; b0 += 64) count(SequenceWork(a, b0 + lane, lane, tokens));
     // A tile of s steps becomes ceil(s / step) items, half of one more than s / step on average.  Shared tiles take the GPU for
-    // long: their items are to fit one round, two where the tiles alone nearly fill one; many tiles are split where one has
-    // more than its share of two rounds.
+    // long: their items are to fit one round, two where the tiles alone fill more than half of one; many tiles are split where one
+    // has more than its share of two rounds.  us in one round / two, 32 q / 8 kv heads behind 32768 tokens (32 heads behind 4096 in
+    // parentheses), tiles over places: 0.49 813 / 816 (138 / 155), 0.54 1124 / 949 (235 / 172), 0.62 1147 / 1046; two rounds less the
+    // halves / two rounds: 1.1 1915 / 1918 (350 / 411), 1.3 2883 / 2137 (453 / 473).
     float wanted = (float)a.parts_wanted;
-    if (!SIDE) wanted = tiles > 1.2f * wanted ? 2.f * wanted : (tiles > 0.6f * wanted ? 2.f : 1.f) * wanted - 0.5f * tiles;
+    if (!SIDE) wanted = tiles > 1.2f * wanted ? 2.f * wanted : (tiles > 0.5f * wanted ? 2.f : 1.f) * wanted - 0.5f * tiles;
     it.step = __builtin_amdgcn_readfirstlane(max(SIDE ? kSideLeast : kSharedLeast, (int)ceilf(all / wanted)));
     it.stream = all * (float)a.n_kv_heads * (2.f * kSideStep * kRowBytes) >= kStreamBytes;
   }
