@@ -288,7 +288,7 @@ int fier_decode_step_phase(const fier_config *cfg, const fier_cache *layers, int
  * to a sum that is not), the outputs once at the end.  sm_scale may have any sign; sm_scale * log2(e) must be finite in
  * binary32 (FIER_EINVAL).  Integer arrays are 4-byte aligned.
  * k and v must be finite as K and V are: a value of v that is not reaches the outputs of tokens in front of it too, since it
- * meets their weights of 0.  Logits and 256 times the sum of |v| over a sequence's rows must lie within binary32.
+ * meets their weights of 0.  q . k, logits and 256 times the sum of |v| over a sequence's rows must lie within binary32.
  */
 
 /* Causal attention of whole prompts: token i of a sequence attends over its tokens 0 .. i.  No cache and no workspace.  Of

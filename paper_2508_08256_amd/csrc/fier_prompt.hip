@@ -268,8 +268,9 @@ struct Rows32 {
     for (int i = 0; i < 16; ++i) l += s[i];
   }
 
-  // The weights, rounded to the K dtype (to nearest: with bf16 by 2^-9 of each at most, about as much again in the sum of many as
-  // the rounding of the output; three exact parts as in the decode step would make it three products), times V.
+  // The weights, rounded to the K dtype (to nearest, at most half a step: 2^-8 of each with bf16, 2^-11 with fp16), times V.  Against 64
+  // bits the outputs of whole prompts are off by a fifth more than with unrounded weights, whose outputs are rounded all the same (bf16
+  // 1.6e-3 -> 1.9e-3 relative, fp16 2.0e-4 -> 2.3e-4); three exact parts as in the decode step would make it three products.
   __device__ __forceinline__ void add_values(const LdsReads& r, int at, const floatx16_t& p) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -630,7 +631,8 @@ struct SharedTile {
 
 // ---- shared tiles in several parts: a second launch joins them ------------------------------------------------------------------
 // Joined by the last workgroup of each tile, as the side-by-side ones are, it was one CU that read up to 3 MB: 64 tokens of 32 q / 8 kv
-// heads behind 32768 took 93 us, now 62 to 69.
+// heads behind 32768 took 93 us, now 56 with the rows in the last cache and 69 without.  (Still twice what the bytes need: 94 partial
+// results a head of 67.6 KB each, 51 MB written and read again beside 134 MB of K and V.)
 // Per wavefront o as the lanes hold it, 16 chunks of 64 x 4 floats (channel tile ct, channels 8 i + 4 h + 0..3: chunk 4 ct + i),
 // then m and l of the lanes.
 __device__ __forceinline__ float* shared_slot(const PromptArgs& a, const Item& it, int head, int turned, int part) {
