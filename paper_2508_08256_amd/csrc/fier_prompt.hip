@@ -286,20 +286,32 @@ struct Rows32 {
   }
 };
 
-// Two outputs.  A mean of V lies within V's type, but rounded weights over a sum that is not can make it larger by 2^-11 (fp16):
-// past 65520 it would become an infinity.  (bf16 values that large are outside what the sums can hold.)
-template <int DT>
-__device__ __forceinline__ uint32_t pack2_outputs(float a, float b) {
+// A mean of V lies within V's type, but rounded weights over a sum that is not can make it larger by 2^-11 (fp16): past 65520 it
+// would be rounded to an infinity, and is held at the largest value.  What is an infinity or a NaN before it is rounded stays one.  (bf16
+// values that large are outside what the sums can hold.)  Behind a branch that ordinary values never take: with three instructions for
+// every value a prompt of 100 tokens took 7.5 us instead of 7.3.
+template <int DT, int N>
+__device__ __forceinline__ void hold_overflows(float (&o)[N]) {
   constexpr float kMost = 65504.f;
-  if (DT == DT_F16) return pack2<DT>(__builtin_amdgcn_fmed3f(a, -kMost, kMost), __builtin_amdgcn_fmed3f(b, -kMost, kMost));
-  return pack2<DT>(a, b);
+  if (DT != DT_F16) return;
+  float mx = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) mx = fmaxf(mx, fabsf(o[i]));
+  if (__builtin_expect(__any(mx > kMost), 0)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = __builtin_isfinite(o[i]) ? __builtin_amdgcn_fmed3f(o[i], -kMost, kMost) : o[i];
+  }
 }
 template <int DT>
 __device__ __forceinline__ void store_channels(char* out_row, int ct, int h, const floatx16_t& o, float inv) {
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = o[i] * inv;
+  hold_overflows<DT>(y);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     *reinterpret_cast<uint2*>(out_row + ct * 64 + i * 16 + h * 8) =
-        make_uint2(pack2_outputs<DT>(o[4 * i] * inv, o[4 * i + 1] * inv), pack2_outputs<DT>(o[4 * i + 2] * inv, o[4 * i + 3] * inv));
+        make_uint2(pack2<DT>(y[4 * i], y[4 * i + 1]), pack2<DT>(y[4 * i + 2], y[4 * i + 3]));
 }
 
 // ---- one query row per lane and half ------------------------------------------------------------------------------------
@@ -695,11 +707,17 @@ __device__ __forceinline__ void join_chunks(const PromptArgs& a, const Item& it,
     }
     const QueryRow row(a, it.sp, head, t.tile * kRowTile + (c >> 4) * 32 + (lane & 31), it.sp.n * a.n_rep);
     const float inv = l > 0.f ? 1.f / l : 0.f;
+    float y[4 * CH];
+#pragma unroll
+    for (int x = 0; x < CH; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[4 * x + i] = o[x][i] * inv;
+    hold_overflows<DT>(y);
     if (row.there) {
 #pragma unroll
       for (int x = 0; x < CH; ++x)
         *reinterpret_cast<uint2*>(row.out + ((c & 15) + x) * 16 + (lane >> 5) * 8) =
-            make_uint2(pack2_outputs<DT>(o[x][0] * inv, o[x][1] * inv), pack2_outputs<DT>(o[x][2] * inv, o[x][3] * inv));
+            make_uint2(pack2<DT>(y[4 * x], y[4 * x + 1]), pack2<DT>(y[4 * x + 2], y[4 * x + 3]));
     }
   }
 }

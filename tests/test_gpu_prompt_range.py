@@ -66,3 +66,25 @@ def test_rows_without_a_token_so_far_do_not_round_the_logits_of_others(dtype, fi
     want = torch.softmax(torch.where(seen, cfg.sm_scale * (j % 4).double(), -math.inf), dim=1) @ v[:, 0].double()
     u = torch.finfo(q.dtype).eps / 2
     assert bool(((out - want).abs() <= (2 * u + u * u + 1e-5) * want).all()), float(((out - want) / want.clamp(min=1e-9)).abs().max())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("first,new", [(None, 20), (None, 200), (0, 200), (3000, 3)])
+def test_values_that_are_not_finite_show(dtype, bad, first, new):
+    """They may not be passed; if one is, the outputs of the rows that attend over it say so."""
+    rows = new + (first or 0)
+    cap = -(-rows // 64) * 64
+    cfg = B.make_config(1, 1, 1, cap, dtype)
+    q, k, v = (torch.ones(n, 1, D, dtype=torch.float16 if dtype == F16 else torch.bfloat16) for n in (new, rows, rows))
+    v[rows - 2, 0, 5] = bad
+    if first is None:
+        out = run_prefill(cfg, q, k, v, [new])
+    else:
+        dev = [torch.zeros(1, cap, D, dtype=q.dtype, device="cuda") for _ in range(2)]
+        for d, s in zip(dev, (k, v)):
+            d[0, :rows] = s[:, 0].cuda()
+        out = run_chunk(cfg, B.DeviceCache(cfg, *dev, i32([first])), q, [new])
+    seen = out[new - 2:, 0, 5].float()
+    assert not bool(seen.isfinite().any())
+    assert bool((out[:, 0, :5] == 1).all())  # equal weights, exact sums: the mean of ones
