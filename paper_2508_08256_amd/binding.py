@@ -475,7 +475,8 @@ def append_chunk(cfg: Config, cache: DeviceCache, k_new, v_new, starts, max_new:
 def block_table(cfg: Config, block_tokens: int, old_lens, new_lens, table, free_blocks, n_free, n_free_out, starts=None,
                 slots=None):
     """int32 tensors on the GPU: old_lens, new_lens [batch], table [batch][max_ctx / block_tokens], free_blocks [pool blocks],
-    n_free, n_free_out of one element, starts [batch + 1], slots of any size."""
+    n_free, n_free_out of one element, starts [batch + 1], slots of any size.  n_free_out negative: too few blocks, nothing has changed
+    but starts, with which no sequence has tokens."""
     int32, on_gpu = _torch_types()[2], True
     for t in (old_lens, new_lens, table, free_blocks, n_free, n_free_out, starts, slots):
         if t is not None:
